@@ -70,6 +70,7 @@ extern "C" {
 #define LT_STATUS_TIMEOUT 1  /* a bounded device-side wait ran out; results are invalid   */
 #define LT_STATUS_FALLBACK 2 /* some rows took the exact unfused fallback (informational) */
 #define LT_STATUS_BOUNDS 4   /* a debug bounds check failed                               */
+#define LT_STATUS_SHORT 8    /* lt_page_tables: the step does not fit (pages, table columns or rows of the batch) */
 
 #define LT_MAX_TOPK 8192
 #define LT_BINS 256 /* m, the number of equal-width score bins (paper Sec. 3.2, "Sampling") */
@@ -266,10 +267,114 @@ int lt_knn_scores(int dtype, const void* q, const void* x, int T, int N, int D,
  * All pointers are device memory: idx [T][topk] int32 (entries < 0 or >= N are skipped), union_pos
  * [ceil(T / group)][group * topk] int32, union_len [ceil(T / group)] int32, member_mask
  * [T][ceil(group * topk / 32)] uint32.  1 <= group, group * topk <= 2^24.  Integer work only: the
- * result is exact.  The masked attention that consumes these is not part of this library.
+ * result is exact.  (The attention over each row's own positions is lt_kv4_attention_topk.)
  */
 int lt_dsa_union_mask(const int32_t* idx, int T, int topk, int N, int group,
                       int32_t* union_pos, int32_t* union_len, uint32_t* member_mask, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * A serving step over a key-value cache held in 4 bits (no counterpart in the paper, which leaves the cache and the attention
+ * over the selected positions to its serving engine, Sec. 4.1).  One step is
+ *     lt_page_tables            where the step's tokens go, from the requests' lengths
+ *     lt_kv4_append             their keys and values into the cache
+ *     lt_indexer_topk_paged     (sparse attention) the positions each token reads; row b of page_table is request b's table
+ *     lt_kv4_attention          causal attention over all positions, or
+ *     lt_kv4_attention_topk     over the selected ones
+ * All lengths live on the device: the calls of a step can be captured into one CUDA graph and replayed as the requests grow.
+ *
+ * Cache.  A pool of pages of LT_PAGE_KEYS = 64 tokens; page p holds, for each of Hkv key-value heads, 64 rows of D + D / 8
+ * bytes, so a page takes lt_kv4_page_bytes(Hkv, D) bytes and row `slot` of head h starts at byte
+ *     ((slot / 64 * Hkv + h) * 64 + slot % 64) * (D + D / 8)
+ * A row is D / 2 bytes of key codes (element 2 i in the low half of byte i, 2 i + 1 in the high one), D / 2 bytes of value
+ * codes, D / 32 key scales and D / 32 value scales (fp16), one scale per LT_KV4_GROUP = 32 elements.
+ *     scale = fp16(bf16(max |x| / 7)), at most 2048;  code = 8 + clamp(round_half_even(x / scale), -7, 7);
+ *     value = (code - 8) * scale
+ * so values beyond 14,336 saturate, and NaN is stored as 0.  D is 64 or 128.
+ *
+ * Requests.  B of them in consecutive rows of the step's batch: request b has rows query_start[b] .. query_start[b + 1] - 1
+ * (ascending), and row query_start[b] + j stands at position context_len[b] + j.  Rows from query_start[B] on are padding:
+ * no output is written there.  Positions 64 j .. 64 j + 63 of request b lie in page page_table[b][j].  A position whose table
+ * entry is no page of the pool, or lies beyond the table, is seen by no token.
+ * ---------------------------------------------------------------------------------------------
+ */
+#define LT_KV4_GROUP 32
+size_t lt_kv4_page_bytes(int Hkv, int D); /* 0 for a D or Hkv that is not supported */
+
+/*
+ * Block tables, slot map and positions of a step.
+ *   context_len   device, [B] int32: tokens each request has in the cache;  new_len: device, [B] int32: tokens it adds
+ *   free_pages    device, n_free int32 (may be NULL if n_free is 0): pages handed out from the front, to the requests in order
+ *   page_table    device, [B][max_pages] int32, in and out: the columns of the pages that a request needs beyond
+ *                 ceil(context_len / 64) are set, all others left as they are
+ *   total_len     device, [B] int32: context_len + new_len (the next step's context_len)
+ *   query_start   device, [B + 1] int32: exclusive sums of new_len, clipped to T
+ *   slot_map      device, [T] int32: row of the pool of every token of the step;  position: device, [T] int32: its position.
+ *                 Both -1 from row query_start[B] on; a slot is -1 where there is no page for the token
+ *   status8       device, 8 int32: [0] LT_STATUS_SHORT if free pages ran out, a request needs more than max_pages pages, the
+ *                 tokens are more than T, or a length is negative (it counts as 0); [1] tokens of the step, [2] pages handed
+ *                 out (the caller's free list then starts that much later), [3] pages that were missing; the rest 0
+ * Pages that are missing are entered as -1.  total_len must not be context_len or new_len.  Integer work only: exact.
+ */
+int lt_page_tables(const int32_t* context_len, const int32_t* new_len, const int32_t* free_pages, int n_free, int B,
+                   int max_pages, int T, int32_t* page_table, int32_t* total_len, int32_t* query_start, int32_t* slot_map,
+                   int32_t* position, int32_t* status8, void* stream);
+
+/*
+ * Quantises the keys and values of T tokens into their slots.
+ *   dtype         LT_DTYPE_BF16 or LT_DTYPE_F32: type of k and v
+ *   k, v          device: token t's Hkv heads of D elements are dense at k + t * k_stride (elements; strides may differ, such as
+ *                 for parts of a fused projection).  Pointers and rows 16-byte aligned
+ *   slot_map      device, [T] int32; tokens whose slot is negative or beyond the pool are skipped.  Slots must differ: what a
+ *                 slot holds that is named twice is undefined
+ *   pool          device, 16-byte aligned, pool_pages * lt_kv4_page_bytes(Hkv, D) bytes; rows of other slots are left as they are
+ */
+int lt_kv4_append(int dtype, const void* k, const void* v, long long k_stride, long long v_stride, const int32_t* slot_map,
+                  int T, int Hkv, int D, void* pool, long long pool_pages, void* stream);
+
+/*
+ * Reads n slots back: k_out, v_out (device, [n][Hkv][D], dense, 16-byte aligned, dtype LT_DTYPE_BF16 or LT_DTYPE_F32) get the
+ * values that the cache holds, rounded to dtype; zeros for a slot that is negative or beyond the pool.  A slot may be named
+ * any number of times.
+ */
+int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t* slots, int n, int Hkv, int D, void* k_out,
+                void* v_out, void* stream);
+
+/*
+ * Causal attention of a step's tokens over their requests' cached positions, their own among them (append first):
+ *     out[t][h] = sum_s softmax_s(scale * q[t][h] . k[s][h / (Hq / Hkv)]) v[s][h / (Hq / Hkv)],   s = 0 .. position of t
+ *     lse[t][h] = log sum_s exp(scale * q[t][h] . k[s])          (natural logarithm; to join with parts attended elsewhere)
+ * A token that sees nothing gets 0 and -inf.
+ *   dtype         LT_DTYPE_BF16 (tensor cores) or LT_DTYPE_F32 (LT_PATH_GENERIC: fp32 arithmetic); type of q and out
+ *   q             device: token t's Hq heads of D elements are dense at q + t * q_stride (elements); pointer and rows 16-byte
+ *                 aligned.  Hq a multiple of Hkv
+ *   out, lse      device, [T][Hq][D] and [T][Hq] fp32 (or NULL), out 16-byte aligned
+ *   max_new       most tokens that any request adds in this step, or 0 if unknown.  It only decides which kernels are
+ *                 launched; results do not depend on it
+ *   scale         any finite number
+ *   workspace     device, 256-byte aligned, at least lt_kv4_attention_workspace_bytes(...) bytes, scratch; one per stream
+ *   tunables      path (AUTO, FUSED, GENERIC), grid and wait_limit_us are used; NULL = defaults
+ * q, and the keys and values of positions that some token sees, must be finite; what lies anywhere else in the pool is not
+ * used, whatever it is.  Probabilities are rounded to fp16 for the products with the values, everything else is held in fp32;
+ * results do not depend on the run (no atomics), but their last bits may on the lengths of the other requests of the batch.
+ */
+int lt_kv4_attention(int dtype, const void* q, long long q_stride, const void* pool, long long pool_pages,
+                     const int32_t* page_table, int max_pages, const int32_t* query_start, const int32_t* context_len, int B,
+                     int T, int Hq, int Hkv, int D, int max_new, float scale, void* out, float* lse, void* workspace,
+                     size_t workspace_bytes, const lt_tunables* tunables, void* stream);
+
+/*
+ * The same over idx[t][0 .. topk) (device, [T][topk] int32, as the top-k entry points write it: positions of t's own
+ * request).  Entries that are negative or beyond t's own position are skipped, wherever they stand; a position that is named
+ * twice counts twice.  1 <= topk <= LT_MAX_TOPK.
+ */
+int lt_kv4_attention_topk(int dtype, const void* q, long long q_stride, const void* pool, long long pool_pages,
+                          const int32_t* page_table, int max_pages, const int32_t* query_start, const int32_t* context_len,
+                          const int32_t* idx, int topk, int B, int T, int Hq, int Hkv, int D, float scale, void* out, float* lse,
+                          void* workspace, size_t workspace_bytes, const lt_tunables* tunables, void* stream);
+
+/* Bytes of workspace that either form needs on the current device (0 on invalid or unsupported arguments). */
+size_t lt_kv4_attention_workspace_bytes(int dtype, int T, int B, int Hq, int Hkv, int D);
 
 /*
  * Host-only helper (no GPU work): the sample plan the fused path would use for this problem.

@@ -18,6 +18,12 @@ from .binding import (  # noqa: F401
     lt_indexer_topk_ex,
     lt_indexer_topk_static,
     lt_indexer_topk_workspace_bytes,
+    lt_kv4_append,
+    lt_kv4_attention,
+    lt_kv4_attention_topk,
+    lt_kv4_attention_workspace_bytes,
+    lt_kv4_read,
+    lt_page_tables,
     lt_read_status,
     lt_unfused_topk,
 )

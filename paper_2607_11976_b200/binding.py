@@ -18,9 +18,10 @@ from . import build as _build
 LT_DTYPE_F32, LT_DTYPE_BF16, LT_DTYPE_E4M3 = 0, 1, 2
 LT_PATH_AUTO, LT_PATH_FUSED, LT_PATH_GENERIC, LT_PATH_FUSED_ABS = 0, 1, 2, 3
 LT_OK = 0
-LT_STATUS_TIMEOUT, LT_STATUS_FALLBACK, LT_STATUS_BOUNDS = 1, 2, 4
+LT_STATUS_TIMEOUT, LT_STATUS_FALLBACK, LT_STATUS_BOUNDS, LT_STATUS_SHORT = 1, 2, 4, 8
 LT_DEBUG_SKIP_ONE_KTILE, LT_DEBUG_SKIP_SAMPLE_KTILE = 1, 2
 LT_MAX_TOPK = 8192
+LT_PAGE_KEYS, LT_KV4_GROUP = 64, 32
 
 _DTYPE_CODES = {"f32": LT_DTYPE_F32, "bf16": LT_DTYPE_BF16, "e4m3": LT_DTYPE_E4M3}
 
@@ -114,6 +115,21 @@ def load() -> ctypes.CDLL:
     lib.lt_indexer_topk_strided.argtypes = [i, vp, fp, vp, ctypes.c_longlong, fp, i, i, i, i, i, i, ip, fp, vp, sz,
                                             ctypes.POINTER(Tunables), vp]
     lib.lt_indexer_topk_strided.restype = i
+    ll, fl, tun = ctypes.c_longlong, ctypes.c_float, ctypes.POINTER(Tunables)
+    lib.lt_kv4_page_bytes.argtypes = [i, i]
+    lib.lt_kv4_page_bytes.restype = sz
+    lib.lt_page_tables.argtypes = [ip, ip, ip, i, i, i, i, ip, ip, ip, ip, ip, ip, vp]
+    lib.lt_page_tables.restype = i
+    lib.lt_kv4_append.argtypes = [i, vp, vp, ll, ll, ip, i, i, i, vp, ll, vp]
+    lib.lt_kv4_append.restype = i
+    lib.lt_kv4_read.argtypes = [i, vp, ll, ip, i, i, i, vp, vp, vp]
+    lib.lt_kv4_read.restype = i
+    lib.lt_kv4_attention.argtypes = [i, vp, ll, vp, ll, ip, i, ip, ip, i, i, i, i, i, i, fl, vp, fp, vp, sz, tun, vp]
+    lib.lt_kv4_attention.restype = i
+    lib.lt_kv4_attention_topk.argtypes = [i, vp, ll, vp, ll, ip, i, ip, ip, ip, i, i, i, i, i, i, fl, vp, fp, vp, sz, tun, vp]
+    lib.lt_kv4_attention_topk.restype = i
+    lib.lt_kv4_attention_workspace_bytes.argtypes = [i, i, i, i, i, i]
+    lib.lt_kv4_attention_workspace_bytes.restype = sz
     lib.lt_launch_count.restype = ctypes.c_ulonglong
     lib.lt_set_profiling.argtypes = [i]
     lib.lt_set_profiling.restype = i
@@ -285,6 +301,120 @@ def lt_dsa_union_mask(idx, N: int, group: int, union_pos, union_len, member_mask
     T, topk = idx.shape
     _check(load().lt_dsa_union_mask(_ptr(idx), T, topk, N, group, _ptr(union_pos), _ptr(union_len), _ptr(member_mask),
                                     _stream(stream)), "lt_dsa_union_mask")
+
+
+# ---------------------------------------------------------------------------------------------
+# serving step over a key-value cache held in 4 bits
+# ---------------------------------------------------------------------------------------------
+
+def _rows(t: torch.Tensor, dtype) -> tuple:
+    """(pointer, row stride in elements) of a [T, H, D] CUDA view whose heads are dense."""
+    want = (torch.float32,) if dtype_code(dtype) == LT_DTYPE_F32 else (torch.bfloat16,)
+    if t.dim() != 3 or not t.is_cuda or t.dtype not in want or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError("expected a [T, H, D] CUDA tensor of the call's dtype with dense heads")
+    return t.data_ptr(), int(t.stride(0)) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _ints(*tensors) -> None:
+    for t in tensors:
+        if t is not None and t.dtype != torch.int32:
+            raise ValueError("expected int32 tensors")
+
+
+def _pool_shape(pool: torch.Tensor) -> tuple:
+    """(pages, key-value heads, D) of a pool uint8 [pages, Hkv, 64, D + D / 8]."""
+    if pool.dim() != 4 or pool.dtype != torch.uint8 or pool.shape[2] != LT_PAGE_KEYS or pool.shape[3] % 9 != 0:
+        raise ValueError("expected a pool uint8 [pages, Hkv, 64, D + D / 8]")
+    return pool.shape[0], pool.shape[1], pool.shape[3] // 9 * 8
+
+
+def lt_kv4_page_bytes(Hkv: int, D: int) -> int:
+    return int(load().lt_kv4_page_bytes(Hkv, D))
+
+
+def alloc_kv4_pool(pages: int, Hkv: int, D: int, device="cuda") -> torch.Tensor:
+    """An empty pool: uint8 [pages, Hkv, 64, D + D / 8], the shape that the calls below take Hkv and D from."""
+    if lt_kv4_page_bytes(Hkv, D) == 0:
+        raise ValueError("unsupported Hkv or D")
+    return torch.empty((pages, Hkv, LT_PAGE_KEYS, D + D // 8), dtype=torch.uint8, device=device)
+
+
+def lt_page_tables(context_len, new_len, free_pages, page_table, total_len, query_start, slot_map, position, status,
+                   stream=None) -> None:
+    """Block tables, slot map and positions of a step: int32 CUDA tensors context_len [B], new_len [B], free_pages
+    [n_free], page_table [B, max_pages] (in and out), total_len [B], query_start [B + 1], slot_map [T], position [T],
+    status [8]."""
+    B, T = context_len.numel(), slot_map.numel()
+    _ints(context_len, new_len, free_pages, page_table, total_len, query_start, slot_map, position, status)
+    if (new_len.numel() != B or page_table.dim() != 2 or page_table.shape[0] != B or total_len.numel() != B or
+            query_start.numel() != B + 1 or position.numel() != T or status.numel() < 8):
+        raise ValueError("the tables disagree on the number of requests or tokens")
+    n_free = 0 if free_pages is None else free_pages.numel()
+    _check(load().lt_page_tables(_ptr(context_len), _ptr(new_len), _ptr(free_pages) if n_free else None, n_free, B,
+                                 page_table.shape[1], T, _ptr(page_table), _ptr(total_len), _ptr(query_start), _ptr(slot_map),
+                                 _ptr(position), _ptr(status), _stream(stream)), "lt_page_tables")
+
+
+def lt_kv4_append(dtype, k, v, slot_map, pool, stream=None) -> None:
+    """Quantises k, v [T, Hkv, D] (rows may be strided) into the slots of the pool."""
+    pages, Hkv, D = _pool_shape(pool)
+    if k.shape != v.shape or tuple(k.shape[1:]) != (Hkv, D) or slot_map.numel() != k.shape[0]:
+        raise ValueError("k, v, slot_map and pool disagree")
+    _ints(slot_map)
+    (kp, ks), (vp_, vs) = _rows(k, dtype), _rows(v, dtype)
+    _check(load().lt_kv4_append(dtype_code(dtype), kp, vp_, ks, vs, _ptr(slot_map), k.shape[0], Hkv, D, _ptr(pool), pages,
+                                _stream(stream)), "lt_kv4_append")
+
+
+def lt_kv4_read(dtype, pool, slots, k_out, v_out, stream=None) -> None:
+    """Values of the slots as k_out, v_out [n, Hkv, D]."""
+    pages, Hkv, D = _pool_shape(pool)
+    if k_out.shape != v_out.shape or tuple(k_out.shape) != (slots.numel(), Hkv, D):
+        raise ValueError("slots, outputs and pool disagree")
+    _ints(slots)
+    _rows(k_out, dtype), _rows(v_out, dtype)
+    _check(load().lt_kv4_read(dtype_code(dtype), _ptr(pool), pages, _ptr(slots), slots.numel(), Hkv, D, _ptr(k_out),
+                              _ptr(v_out), _stream(stream)), "lt_kv4_read")
+
+
+def lt_kv4_attention_workspace_bytes(dtype, T: int, B: int, Hq: int, Hkv: int, D: int) -> int:
+    return int(load().lt_kv4_attention_workspace_bytes(dtype_code(dtype), T, B, Hq, Hkv, D))
+
+
+def _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse):
+    pages, Hkv, D = _pool_shape(pool)
+    T, Hq = q.shape[0], q.shape[1]
+    B = context_len.numel()
+    if (q.dim() != 3 or q.shape[2] != D or out.shape != q.shape or out.dtype != q.dtype or page_table.dim() != 2 or
+            page_table.shape[0] != B or query_start.numel() != B + 1 or
+            (out_lse is not None and (out_lse.numel() != T * Hq or out_lse.dtype != torch.float32))):
+        raise ValueError("q, pool, tables and outputs disagree")
+    _ints(page_table, query_start, context_len)
+    qp, qs = _rows(q, dtype)
+    return pages, Hkv, D, T, Hq, B, qp, qs
+
+
+def lt_kv4_attention(dtype, q, pool, page_table, query_start, context_len, scale: float, out, out_lse, workspace,
+                     max_new: int = 0, tunables: Optional[Tunables] = None, stream=None) -> None:
+    """Causal attention of q [T, Hq, D] over the requests' pages (out [T, Hq, D], out_lse fp32 [T, Hq] or None)."""
+    pages, Hkv, D, T, Hq, B, qp, qs = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse)
+    _check(load().lt_kv4_attention(dtype_code(dtype), qp, qs, _ptr(pool), pages, _ptr(page_table), page_table.shape[1],
+                                   _ptr(query_start), _ptr(context_len), B, T, Hq, Hkv, D, max_new, scale, _ptr(out),
+                                   _ptr(out_lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                   ctypes.byref(tunables) if tunables else None, _stream(stream)), "lt_kv4_attention")
+
+
+def lt_kv4_attention_topk(dtype, q, pool, page_table, query_start, context_len, idx, scale: float, out, out_lse, workspace,
+                          tunables: Optional[Tunables] = None, stream=None) -> None:
+    """The same over the positions idx [T, topk] (int32, as lt_indexer_topk_paged writes them)."""
+    pages, Hkv, D, T, Hq, B, qp, qs = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse)
+    if idx.dim() != 2 or idx.shape[0] != T:
+        raise ValueError("expected idx [T, topk]")
+    _ints(idx)
+    _check(load().lt_kv4_attention_topk(dtype_code(dtype), qp, qs, _ptr(pool), pages, _ptr(page_table), page_table.shape[1],
+                                        _ptr(query_start), _ptr(context_len), _ptr(idx), idx.shape[1], B, T, Hq, Hkv, D, scale,
+                                        _ptr(out), _ptr(out_lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                        ctypes.byref(tunables) if tunables else None, _stream(stream)), "lt_kv4_attention_topk")
 
 
 def lt_indexer_scores(dtype, q, w, k, k_scale, causal_offset: int, row_begin: int, row_end: int, out_scores,

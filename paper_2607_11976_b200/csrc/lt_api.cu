@@ -12,6 +12,7 @@
 #include "../../include/lt_indexer.h"
 #include "lt_common.cuh"
 #include "lt_host.h"
+#include "lt_kv4.cuh"
 #include "lt_work_items.h"
 
 namespace lt {
@@ -797,6 +798,117 @@ int lt_dsa_union_mask(const int32_t* idx, int T, int topk, int N, int group, int
     return LT_ERR_INVALID_ARG;
   LT_LAUNCH(launch_dsa_union(idx, T, topk, N, group, union_pos, union_len, member_mask, static_cast<cudaStream_t>(stream)));
   return LT_OK;
+}
+
+// ---- serving step over the 4-bit cache ---------------------------------------------------------------------------------
+static bool kv4_shape(int Hkv, int D) { return Hkv > 0 && Hkv <= 1024 && (D == 64 || D == 128); }
+static bool kv4_dtype(int dtype) { return dtype == LT_DTYPE_BF16 || dtype == LT_DTYPE_F32; }
+// slots are int32
+static bool kv4_pool(const void* pool, long long pages) {
+  return pool != nullptr && aligned16(pool) && pages > 0 && pages <= INT_MAX / kPageKeys;
+}
+
+size_t lt_kv4_page_bytes(int Hkv, int D) {
+  return kv4_shape(Hkv, D) ? static_cast<size_t>(Hkv) * kPageKeys * kv4_row_bytes(D) : 0;
+}
+
+int lt_page_tables(const int32_t* context_len, const int32_t* new_len, const int32_t* free_pages, int n_free, int B,
+                   int max_pages, int T, int32_t* page_table, int32_t* total_len, int32_t* query_start, int32_t* slot_map,
+                   int32_t* position, int32_t* status8, void* stream) {
+  if (context_len == nullptr || new_len == nullptr || page_table == nullptr || total_len == nullptr || query_start == nullptr ||
+      slot_map == nullptr || position == nullptr || status8 == nullptr || n_free < 0 || (n_free > 0 && free_pages == nullptr) ||
+      B <= 0 || B > (1 << 20) || max_pages <= 0 || max_pages > INT_MAX / kPageKeys || T <= 0 || total_len == context_len ||
+      total_len == new_len)
+    return LT_ERR_INVALID_ARG;
+  LT_LAUNCH(launch_page_tables(context_len, new_len, free_pages, n_free, B, max_pages, T, page_table, total_len, query_start,
+                               slot_map, position, status8, static_cast<cudaStream_t>(stream)));
+  return LT_OK;
+}
+
+int lt_kv4_append(int dtype, const void* k, const void* v, long long k_stride, long long v_stride, const int32_t* slot_map,
+                  int T, int Hkv, int D, void* pool, long long pool_pages, void* stream) {
+  if (!kv4_dtype(dtype) || (Hkv > 0 && !kv4_shape(Hkv, D))) return LT_ERR_UNSUPPORTED;
+  const long long per16 = 16 / static_cast<long long>(elem_bytes(dtype));
+  if (k == nullptr || v == nullptr || slot_map == nullptr || T <= 0 || Hkv <= 0 || !kv4_pool(pool, pool_pages) || !aligned16(k) ||
+      !aligned16(v) || k_stride < static_cast<long long>(Hkv) * D || v_stride < static_cast<long long>(Hkv) * D ||
+      k_stride % per16 != 0 || v_stride % per16 != 0)
+    return LT_ERR_INVALID_ARG;
+  LT_LAUNCH(launch_kv4_append(dtype, k, v, k_stride, v_stride, slot_map, T, Hkv, D, pool, pool_pages, static_cast<cudaStream_t>(stream)));
+  return LT_OK;
+}
+
+int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t* slots, int n, int Hkv, int D, void* k_out,
+                void* v_out, void* stream) {
+  if (!kv4_dtype(dtype) || (Hkv > 0 && !kv4_shape(Hkv, D))) return LT_ERR_UNSUPPORTED;
+  if (slots == nullptr || k_out == nullptr || v_out == nullptr || n <= 0 || Hkv <= 0 || !kv4_pool(pool, pool_pages) ||
+      !aligned16(k_out) || !aligned16(v_out))
+    return LT_ERR_INVALID_ARG;
+  LT_LAUNCH(launch_kv4_read(dtype, pool, pool_pages, slots, n, Hkv, D, k_out, v_out, static_cast<cudaStream_t>(stream)));
+  return LT_OK;
+}
+
+static int kv4_attention_impl(int dtype, const void* q, long long q_stride, const void* pool, long long pool_pages,
+                              const int32_t* page_table, int max_pages, const int32_t* query_start, const int32_t* context_len,
+                              const int32_t* idx, int topk, int B, int T, int Hq, int Hkv, int D, int max_new, float scale,
+                              void* out, float* lse, void* workspace, size_t workspace_bytes, const lt_tunables* tunables,
+                              cudaStream_t stream) {
+  if (!kv4_dtype(dtype) || (Hkv > 0 && !kv4_shape(Hkv, D))) return LT_ERR_UNSUPPORTED;
+  if (q == nullptr || page_table == nullptr || query_start == nullptr || context_len == nullptr || out == nullptr || Hkv <= 0 ||
+      !kv4_pool(pool, pool_pages) || max_pages <= 0 || max_pages > INT_MAX / kPageKeys || B <= 0 || B > (1 << 20) || T <= 0 || Hq <= 0 || Hq % Hkv != 0 ||
+      Hq > 65535 || max_new < 0 || !isfinite(scale) || !aligned16(q) || !aligned16(out) ||
+      q_stride < static_cast<long long>(Hq) * D || q_stride % (16 / static_cast<long long>(elem_bytes(dtype))) != 0)
+    return LT_ERR_INVALID_ARG;
+  const Tun tun = resolve_tunables(tunables);
+  if (tun.path != LT_PATH_AUTO && tun.path != LT_PATH_FUSED && tun.path != LT_PATH_GENERIC) return LT_ERR_INVALID_ARG;
+  if (dtype == LT_DTYPE_F32 && tun.path == LT_PATH_FUSED) return LT_ERR_UNSUPPORTED;
+  if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & (kAlign - 1)) != 0 ||
+      workspace_bytes < lt_kv4_attention_workspace_bytes(dtype, T, B, Hq, Hkv, D))
+    return LT_ERR_WORKSPACE;
+  Kv4AttnParams p{};
+  p.q = q;
+  p.q_stride = q_stride;
+  p.pool = static_cast<const uint8_t*>(pool);
+  p.pool_pages = pool_pages;
+  p.page_table = page_table;
+  p.max_pages = max_pages;
+  p.query_start = query_start;
+  p.context_len = context_len;
+  p.idx = idx;
+  p.topk = topk;
+  p.B = B;
+  p.T = T;
+  p.Hq = Hq;
+  p.Hkv = Hkv;
+  p.group = Hq / Hkv;
+  p.scale = scale;
+  p.out = out;
+  p.lse = lse;
+  p.min_rows = 1;
+  p.max_rows = INT_MAX;
+  LT_LAUNCH(launch_kv4_attention_generic(dtype, D, p, stream));
+  return LT_OK;
+}
+
+int lt_kv4_attention(int dtype, const void* q, long long q_stride, const void* pool, long long pool_pages,
+                     const int32_t* page_table, int max_pages, const int32_t* query_start, const int32_t* context_len, int B,
+                     int T, int Hq, int Hkv, int D, int max_new, float scale, void* out, float* lse, void* workspace,
+                     size_t workspace_bytes, const lt_tunables* tunables, void* stream) {
+  return kv4_attention_impl(dtype, q, q_stride, pool, pool_pages, page_table, max_pages, query_start, context_len, nullptr, 0, B, T,
+                            Hq, Hkv, D, max_new, scale, out, lse, workspace, workspace_bytes, tunables, static_cast<cudaStream_t>(stream));
+}
+
+int lt_kv4_attention_topk(int dtype, const void* q, long long q_stride, const void* pool, long long pool_pages,
+                          const int32_t* page_table, int max_pages, const int32_t* query_start, const int32_t* context_len,
+                          const int32_t* idx, int topk, int B, int T, int Hq, int Hkv, int D, float scale, void* out, float* lse,
+                          void* workspace, size_t workspace_bytes, const lt_tunables* tunables, void* stream) {
+  if (idx == nullptr || topk <= 0 || topk > LT_MAX_TOPK) return LT_ERR_INVALID_ARG;
+  return kv4_attention_impl(dtype, q, q_stride, pool, pool_pages, page_table, max_pages, query_start, context_len, idx, topk, B, T, Hq,
+                            Hkv, D, 0, scale, out, lse, workspace, workspace_bytes, tunables, static_cast<cudaStream_t>(stream));
+}
+
+size_t lt_kv4_attention_workspace_bytes(int dtype, int T, int B, int Hq, int Hkv, int D) {
+  if (!kv4_dtype(dtype) || !kv4_shape(Hkv, D) || T <= 0 || B <= 0 || Hq <= 0 || Hq % Hkv != 0) return 0;
+  return kAlign;
 }
 
 int lt_indexer_sample_plan(int N, int topk, int causal_offset, const lt_tunables* tunables, int plan3[3]) {

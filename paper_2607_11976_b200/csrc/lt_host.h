@@ -295,4 +295,19 @@ cudaError_t launch_gather_keys(const void* k, const float* k_scale, const int32_
 cudaError_t launch_dsa_union(const int32_t* idx, int T, int topk, int N, int group, int32_t* union_pos, int32_t* union_len,
                              uint32_t* mask, cudaStream_t stream);
 
+// ---- lt_kv4_cache.cu ------------------------------------------------------------------------
+cudaError_t launch_page_tables(const int32_t* context_len, const int32_t* new_len, const int32_t* free_pages, int n_free, int B,
+                               int max_pages, int T, int32_t* page_table, int32_t* total_len, int32_t* query_start,
+                               int32_t* slot_map, int32_t* position, int32_t* status, cudaStream_t stream);
+cudaError_t launch_kv4_append(int dtype, const void* k, const void* v, long long k_stride, long long v_stride,
+                              const int32_t* slot_map, int T, int Hkv, int D, void* pool, long long pool_pages,
+                              cudaStream_t stream);
+cudaError_t launch_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t* slots, int n, int Hkv, int D,
+                            void* k_out, void* v_out, cudaStream_t stream);
+
+// ---- lt_kv4_attention.cu: see lt_kv4.cuh ------------------------------------------------------
+struct Kv4AttnParams;
+// One CTA per (token, query head), any head count, fp32 arithmetic throughout.
+cudaError_t launch_kv4_attention_generic(int dtype, int D, const Kv4AttnParams& p, cudaStream_t stream);
+
 }  // namespace lt
