@@ -347,10 +347,10 @@ int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t
  * A token that sees nothing gets 0 and -inf.
  *   dtype         LT_DTYPE_BF16 (tensor cores) or LT_DTYPE_F32 (LT_PATH_GENERIC: fp32 arithmetic); type of q and out
  *   q             device: token t's Hq heads of D elements are dense at q + t * q_stride (elements); pointer and rows 16-byte
- *                 aligned.  Hq a multiple of Hkv
+ *                 aligned.  Hq a multiple of Hkv, T * Hq < 2^31
  *   out, lse      device, [T][Hq][D] and [T][Hq] fp32 (or NULL), out 16-byte aligned
  *   max_new       most tokens that any request adds in this step, or 0 if unknown.  It only decides which kernels are
- *                 launched; results do not depend on it
+ *                 launched: any value is safe, a right one is fastest
  *   scale         any finite number
  *   workspace     device, 256-byte aligned, at least lt_kv4_attention_workspace_bytes(...) bytes, scratch; one per stream
  *   tunables      path (AUTO, FUSED, GENERIC), grid and wait_limit_us are used; NULL = defaults

@@ -106,14 +106,14 @@ def attend(q, k, v, scale):
 
 
 def attention(q, pool, page_table, query_start, context_len, scale, idx=None):
-    """q float64 [T, Hq, D] over the pool uint8 [pages, Hkv, 64, row].  Returns (out, lse, spread, weight), all float64: spread
-    [T, Hq, D] = sum_s p_s |v_s|, and weight [T, Hq] = the largest scale * sum_d |q_d k_d| of any position seen; both bound what a
-    rounding can do.  Rows that are nobody's are NaN."""
+    """q float64 [T, Hq, D] over the pool uint8 [pages, Hkv, 64, row].  Returns (out, lse, spread, weight, mass), all float64:
+    spread [T, Hq, D] = sum_s p_s |v_s|, weight [T, Hq] = the largest scale * sum_d |q_d k_d| of any position seen, and mass
+    [T, Hq, D] = sum_s |v_s| bound what a rounding can do.  Rows that are nobody's are NaN."""
     T, Hq, D = q.shape
     pages, Hkv = pool.shape[:2]
     group = Hq // Hkv
     out, lse = np.full((T, Hq, D), np.nan), np.full((T, Hq), np.nan)
-    spread, weight = np.full((T, Hq, D), np.nan), np.zeros((T, Hq))
+    spread, weight, mass = np.full((T, Hq, D), np.nan), np.zeros((T, Hq)), np.zeros((T, Hq, D))
     for b in range(len(context_len)):
         ctx, t0, t1 = int(context_len[b]), int(query_start[b]), int(query_start[b + 1])
         if t1 <= t0:
@@ -131,6 +131,7 @@ def attention(q, pool, page_table, query_start, context_len, scale, idx=None):
                     see = np.array([i for i in idx[t] if 0 <= i <= last and ok[i]], np.int64)
                 for j in range(h * group, (h + 1) * group):
                     out[t, j], lse[t, j], spread[t, j] = attend(q[t, j], k[see], v[see], scale)
+                    mass[t, j] = np.abs(v[see]).sum(0)
                     if see.size:
                         weight[t, j] = abs(scale) * (np.abs(k[see]) @ np.abs(q[t, j])).max()
-    return out, lse, spread, weight
+    return out, lse, spread, weight, mass

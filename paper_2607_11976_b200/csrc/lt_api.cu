@@ -855,7 +855,7 @@ static int kv4_attention_impl(int dtype, const void* q, long long q_stride, cons
   if (!kv4_dtype(dtype) || (Hkv > 0 && !kv4_shape(Hkv, D))) return LT_ERR_UNSUPPORTED;
   if (q == nullptr || page_table == nullptr || query_start == nullptr || context_len == nullptr || out == nullptr || Hkv <= 0 ||
       !kv4_pool(pool, pool_pages) || max_pages <= 0 || max_pages > INT_MAX / kPageKeys || B <= 0 || B > (1 << 20) || T <= 0 || Hq <= 0 || Hq % Hkv != 0 ||
-      Hq > 65535 || max_new < 0 || !isfinite(scale) || !aligned16(q) || !aligned16(out) ||
+      Hq > 65535 || static_cast<long long>(T) * Hq > INT_MAX || max_new < 0 || !isfinite(scale) || !aligned16(q) || !aligned16(out) ||
       q_stride < static_cast<long long>(Hq) * D || q_stride % (16 / static_cast<long long>(elem_bytes(dtype))) != 0)
     return LT_ERR_INVALID_ARG;
   const Tun tun = resolve_tunables(tunables);
@@ -885,7 +885,15 @@ static int kv4_attention_impl(int dtype, const void* q, long long q_stride, cons
   p.lse = lse;
   p.min_rows = 1;
   p.max_rows = INT_MAX;
-  LT_LAUNCH(launch_kv4_attention_generic(dtype, D, p, stream));
+  if (dtype == LT_DTYPE_F32 || tun.path == LT_PATH_GENERIC) {
+    LT_LAUNCH(launch_kv4_attention_generic(dtype, D, p, stream));
+    return LT_OK;
+  }
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const long long tokens = idx != nullptr ? 1 : (max_new > 0 && max_new < T ? max_new : T);  // most of any request
+  const int sms = sm_count(), grid = tun.grid > 0 && tun.grid < sms ? tun.grid : sms;
+  LT_LAUNCH(launch_kv4_attention_rows(D, tokens * p.group, p, ws, grid, stream));
+  ++g_launches;  // (two kernels)
   return LT_OK;
 }
 
@@ -908,7 +916,7 @@ int lt_kv4_attention_topk(int dtype, const void* q, long long q_stride, const vo
 
 size_t lt_kv4_attention_workspace_bytes(int dtype, int T, int B, int Hq, int Hkv, int D) {
   if (!kv4_dtype(dtype) || !kv4_shape(Hkv, D) || T <= 0 || B <= 0 || Hq <= 0 || Hq % Hkv != 0) return 0;
-  return kAlign;
+  return dtype == LT_DTYPE_BF16 ? align_up(kv4_rows_scratch_bytes(D)) : kAlign;
 }
 
 int lt_indexer_sample_plan(int N, int topk, int causal_offset, const lt_tunables* tunables, int plan3[3]) {

@@ -305,8 +305,13 @@ cudaError_t launch_kv4_append(int dtype, const void* k, const void* v, long long
 cudaError_t launch_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t* slots, int n, int Hkv, int D,
                             void* k_out, void* v_out, cudaStream_t stream);
 
-// ---- lt_kv4_attention.cu: see lt_kv4.cuh ------------------------------------------------------
+// ---- attention over the 4-bit cache: see lt_kv4.cuh --------------------------------------------
 struct Kv4AttnParams;
+// lt_kv4_attention.cu: bf16 queries, few rows (tokens x heads of a group, at most most_rows for any request or token).  scratch:
+// kv4_rows_scratch_bytes(D) bytes for up to sm_count() CTAs.
+size_t kv4_rows_scratch_bytes(int D);
+cudaError_t launch_kv4_attention_rows(int D, long long most_rows, const Kv4AttnParams& p, void* scratch, int grid, cudaStream_t stream);
+// lt_kv4_generic.cu
 // One CTA per (token, query head), any head count, fp32 arithmetic throughout.
 cudaError_t launch_kv4_attention_generic(int dtype, int D, const Kv4AttnParams& p, cudaStream_t stream);
 

@@ -102,21 +102,24 @@ class Step:
         at most ds = weight * (2^-11 + 64 * 4 * 2^-22) where weight >= scale * sum |q k|; |code| >= 1 for most elements but not
         for all, which the factor 4 on the second term covers.  A probability is then off by the factor e^ds, by 2^-11 for its
         rounding to fp16, and the value by 2^-11 for its own; numerator and denominator both move: 2 ds + 2 * 2^-11, with 2^-20
-        for sums and exponentials, of spread = sum p |v|.  Probabilities under 2^-39 of the largest may vanish, and the
-        result is rounded to bf16 (2^-8 of itself).
+        for sums and exponentials, of spread = sum p |v|.  Probabilities under 2^-29 of the largest are subnormal in
+        fp16, times 2^15 as they are held: their rounding is not relative but up to 2^-25, so 2^-40 of the largest each, which shows in an
+        element whose code is 0 at every key that matters (2^-40 mass, mass = sum |v|; the largest probability is at most the sum).
+        The result is rounded to bf16 (2^-8 of itself).
         fp32 path: ds = weight * (D + 8) 2^-24, sums of n terms, and a result rounded to 2^-24."""
-        ref, ref_lse, spread, weight = kv4.attention(self.q, self.pool, self.table, self.start, self.ctx, self.scale, idx)
+        ref, ref_lse, spread, weight, mass = kv4.attention(self.q, self.pool, self.table, self.start, self.ctx, self.scale, idx)
         end = int(self.start[-1])
         assert np.array_equal(out[end:], np.full_like(out[end:], 7.0)), "rows behind the last request were written"
         if fused:
             ds = weight * (2.0**-11 + 4 * 256 * 2.0**-22)
-            rel, last, sums = 2 * ds + 2 * 2.0**-11 + 2.0**-20, 2.0**-8, 2.0**-20
+            rel, last, sums, lost = 2 * ds + 2 * 2.0**-11 + 2.0**-20, 2.0**-8, 2.0**-20, 2.0**-40
         else:
             n = n_most or int((self.ctx + self.new).max())
             ds = weight * (self.D + 8) * 2.0**-24
             rel, last, sums = 2 * ds + (n + 64) * 2.0**-24, 2.0**-24 if self.dtype == "f32" else 2.0**-8, (n + 64) * 2.0**-24
+            lost = 0.0
         with np.errstate(invalid="ignore"):
-            tol = rel[..., None] * spread + last * (1 + rel[..., None]) * np.abs(ref) + 1e-30
+            tol = rel[..., None] * spread + last * (1 + rel[..., None]) * np.abs(ref) + lost * mass + 1e-30
             err = np.abs(out - ref)
         bad = ~(err[:end] <= tol[:end])
         assert not bad.any(), f"{bad.sum()} of {bad.size} off; worst {np.nanmax(err[:end] / tol[:end]):.2f} of the tolerance, first at {np.argwhere(bad)[0]}"

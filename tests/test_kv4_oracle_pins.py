@@ -84,7 +84,7 @@ def test_attention_brute_force_and_empty_rows():
     pool = kv4.pack_rows(rng.standard_normal((3, 2, 64, 64)).astype(np.float32), rng.standard_normal((3, 2, 64, 64)).astype(np.float32))
     q = rng.standard_normal((3, 4, 64))
     table = np.array([[2, 0], [-1, 1]], np.int32)
-    out, lse, spread, _ = kv4.attention(q, pool, table, [0, 2, 3], [64, 0], 0.125)
+    out, lse, spread, _, mass = kv4.attention(q, pool, table, [0, 2, 3], [64, 0], 0.125)
     keys = [(2, s) for s in range(64)] + [(0, 0), (0, 1)]
     for t, n in ((0, 65), (1, 66)):
         for j in range(4):
@@ -94,8 +94,9 @@ def test_attention_brute_force_and_empty_rows():
                 e = np.exp(0.125 * float(k @ q[t, j]))
                 num, den = num + e * v, den + e
             assert np.allclose(out[t, j], num / den, rtol=1e-12) and np.isclose(lse[t, j], np.log(den), rtol=1e-12)
+    assert (np.abs(out[:2]) <= spread[:2] * (1 + 1e-12)).all() and (spread <= mass * (1 + 1e-12)).all()
     assert (out[2] == 0).all() and np.isneginf(lse[2]).all()  # its only page is no page
     idx = np.array([[64, -1, 0], [99, 65, 65], [0, 1, 2]], np.int32)
-    out, lse, _, _ = kv4.attention(q, pool, table, [0, 2, 3], [64, 0], 0.125, idx)
+    out, lse, _, _, _ = kv4.attention(q, pool, table, [0, 2, 3], [64, 0], 0.125, idx)
     k, v = kv4.unpack_rows(pool[0, 0, 1])
     assert np.allclose(out[1, 0], v) and np.isclose(lse[1, 0], 0.125 * float(k @ q[1, 0]) + np.log(2))
