@@ -9,12 +9,15 @@
 // m16n8k16 product and the query rows as its 8 columns: a group of 8 heads wastes nothing, and the cached operand, which is the one
 // that has to be unpacked, lies in the lanes as it comes out of memory.  (The tensor memory's route would write the unpacked tile
 // to shared memory and read it back, 8 clocks per key and head.)
-//   S^T = K Q^T: lane (g, t) holds keys g and g + 8, of each group of 32 elements the 8 of code word t.  Codes become the bf16 numbers
-//     16 + u by or-ing an exponent; the accumulators start at -24 sum q, so that they end at sum q (u - 8), exact products in fp32,
-//     and the scale of (key, group) multiplies that in fp32.
+//   S^T = K Q^T: lane (g, t) holds keys g and g + 8, of each group of 32 elements the 8 of code word t.  A nibble by itself in the low
+//     bits of an fp16 is u 2^-24, one in the bits above it u 2^-20, subnormal and exact, so that a mask makes operands of codes, and
+//     half of them need no shift.  Queries are scaled by a power of two to fp16's range (exact but for what is under 2^-35 of the row's
+//     largest), those that meet u 2^-20 by a further 1 / 16; the accumulators start at -8 sum q, so that they end at sum q (u - 8),
+//     exact products in fp32, and the scale of (key, group) multiplies that in fp32.
 //   P^T: the accumulators, in fp16, turned by movmatrix.  p is held times 2^15, so that fp16 reaches down to 2^-39 of the largest.
 //   O^T = V^T P^T: lane (g, t) holds elements 16 g .. 16 g + 15 of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9: one scale group, words that pair up
-//     by two byte permutations; (16 + u) s - 24 s is one FMA on fp16 pairs.
+//     by two byte permutations.  A value is (16 + u) s - 24 s, one FMA on fp16 pairs, for the nibbles that are shifted there anyway; for
+//     the others (1024 + u) - 1032 or (1024 + 16 u) / 16 - 72, exact, times s: an FMA more and a shift less, which evens out the pipes.
 //
 // Work is dealt out in units of 32 keys: all units of all (request, key-value head, row tile) items in a row are cut into equal
 // runs, one per warp, whatever the lengths.  A warp has its own ring of cp.async stages and waits for nobody.  Items that it
@@ -29,6 +32,11 @@ namespace {
 
 constexpr int kUnit = 32;          // keys of a unit
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+#ifndef KW1
+#define KW1 12
+#define KW2 8
+#define KST 3
+#endif
 constexpr float kPShift = 15.f;    // probabilities are held times 2^15
 
 template <int D, int NT>
@@ -37,9 +45,9 @@ struct Shape {
   static constexpr int kGroups = D / kKvGroup;
   static constexpr int kRows = 8 * NT;       // query rows of an item
   static constexpr int kTilesD = D / 16;     // 16-row tiles of O^T
-  static constexpr int kWarps = NT == 1 ? 16 : 12;
+  static constexpr int kWarps = NT == 1 ? KW1 : KW2;
   static constexpr int kThreads = kWarps * 32;
-  static constexpr int kStages = 3;
+  static constexpr int kStages = KST;
   static constexpr int kUnitBytes = kUnit * kRow;
   static constexpr int kPartFloats = kRows * (D + 2);  // a part: o[kRows][D], m[kRows], l[kRows]
   static constexpr int kRingBytes = kStages * kUnitBytes;
@@ -63,15 +71,17 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same into accumulators that begin at c.
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
+                                             const float (&c)[4]) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t a) {
   uint32_t d;
@@ -91,21 +101,30 @@ __device__ __forceinline__ void cp_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
 }
 
-// Nibble i of each half of w as the bf16 pair 16 + u / as the fp16 pair 16 + u.
-template <int i>
-__device__ __forceinline__ uint32_t bf16_codes(uint32_t w) {
-  const uint32_t x = i == 0 ? w << 3 : w >> (4 * i - 3);
-  return (x & 0x00780078u) | 0x41804180u;
-}
-template <int i>
-__device__ __forceinline__ uint32_t f16_codes(uint32_t w) {
-  const uint32_t x = i < 2 ? w << (6 - 4 * i) : w >> (4 * i - 6);
-  return (x & 0x03C003C0u) | 0x4C004C00u;
-}
+// Nibbles 0 and 1 of each half of w as fp16 pairs u 2^-24 and u 2^-20; nibbles 2 and 3 are those of w >> 8.
+__device__ __forceinline__ uint32_t codes_low(uint32_t w) { return w & 0x000F000Fu; }
+__device__ __forceinline__ uint32_t codes_high(uint32_t w) { return w & 0x00F000F0u; }
 __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d;
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
   return d;
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// Nibble i of each half of w as the fp16 pair (u - 8) s, rounded once; minus24s = -24 s.
+template <int i>
+__device__ __forceinline__ uint32_t f16_values(uint32_t w, uint32_t s, uint32_t minus24s) {
+  if constexpr (i == 0) return hmul2(hadd2(codes_low(w) | 0x64006400u, 0xE408E408u), s);                // - 1032
+  if constexpr (i == 1) return hmul2(hfma2(codes_high(w) | 0x64006400u, 0x2C002C00u, 0xD480D480u), s);  // / 16 - 72
+  return hfma2(((w >> (4 * i - 6)) & 0x03C003C0u) | 0x4C004C00u, s, minus24s);               // 16 + u
 }
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -114,6 +133,12 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
 __device__ __forceinline__ uint32_t bf162_bits(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Quotient of counts that nearly always fit into 32 bits.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+  return a / b;
 }
 
 // ---- items ----------------------------------------------------------------------------------
@@ -146,9 +171,9 @@ struct Cursor {
     } else {
       w.load(p, b);
     }
-    const long long item = off / w.units;
+    const long long item = quotient(off, w.units);
     unit = static_cast<int>(off - item * w.units);
-    kvh = static_cast<int>(item / w.tiles);
+    kvh = static_cast<int>(quotient(item, w.tiles));
     rt = static_cast<int>(item - static_cast<long long>(kvh) * w.tiles);
   }
   // To the next item (there has to be one).
@@ -208,6 +233,14 @@ __device__ __forceinline__ void write_row4(const Kv4AttnParams& p, int token, in
     p.lse[static_cast<long long>(token) * p.Hq + head] = l > 0.f ? (m - kPShift + log2f(l)) * kLn2 : -INFINITY;
 }
 
+// (o, m, l) and another part of the same row: sums relative to the larger maximum.
+__device__ __forceinline__ void join(float4& o, float& m, float& l, const float4& x, float pm, float pl) {
+  const float mm = fmaxf(m, pm), a = m == -INFINITY ? 0.f : ex2(m - mm), b = pm == -INFINITY ? 0.f : ex2(pm - mm);
+  o = make_float4(o.x * a + x.x * b, o.y * a + x.y * b, o.z * a + x.z * b, o.w * a + x.w * b);
+  l = l * a + pl * b;
+  m = mm;
+}
+
 struct SplitBuffers {
   CtaDesc* desc;   // [grid]
   float* cta;      // [grid][2][kPartFloats]
@@ -221,13 +254,18 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ long long s_first[S::kThreads], s_sums[S::kWarps];
   __shared__ PartDesc s_part[S::kWarps][2];
-  __shared__ unsigned s_seen[S::kWarps][S::kStages];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   chain_wait();
 
   // ---- this warp's run [lo, hi) of all units, and where it begins --------------------------------
   const long long gw = static_cast<long long>(blockIdx.x) * S::kWarps + warp, n_warps = static_cast<long long>(gridDim.x) * S::kWarps;
   long long total = 0, lo, hi;
+  auto cut = [&]() {  // as even as it goes; the remainder is spread over the CTAs
+    const long long even = quotient(total, n_warps);
+    const unsigned rest = static_cast<unsigned>(total - even * n_warps), n = static_cast<unsigned>(n_warps), w = static_cast<unsigned>(gw);
+    lo = even * gw + rest * w / n;  // (rest and w are both under 2^12)
+    hi = even * (gw + 1) + rest * (w + 1) / n;
+  };
   Cursor<D, NT, kTopk> at;
   if constexpr (kTopk) {
     int end = p.query_start[p.B];
@@ -235,9 +273,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
     const int units = (p.topk + kUnit - 1) / kUnit, tiles = (p.group + S::kRows - 1) / S::kRows;
     const long long per = static_cast<long long>(units) * tiles * p.Hkv;
     total = per * end;
-    lo = total * gw / n_warps;
-    hi = total * (gw + 1) / n_warps;
-    if (lo < hi) at.start(p, static_cast<int>(lo / per), lo % per);
+    cut();
+    if (lo < hi) {
+      const long long token = quotient(lo, per);
+      at.start(p, static_cast<int>(token), lo - token * per);
+    }
   } else {
     RequestWork<D, NT> w;
     if (p.B > S::kThreads) {  // the total needs a pass of its own
@@ -253,8 +293,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
       s_first[tid] = before + block_scan<S::kWarps>(mine, sum, s_sums);
       __syncthreads();
       if (p.B <= S::kThreads) total = sum;
-      lo = total * gw / n_warps;
-      hi = total * (gw + 1) / n_warps;
+      cut();
       if (lo < hi && lo >= before && lo < before + sum) {
         int a = 0, e = S::kThreads;  // the last request that begins at or before lo is one with units
         while (e - a > 1) {
@@ -277,6 +316,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
   int fetch_stage = 0;
   // dense: the request's pages, 32 at a time
   int pages = -1, pages_at = -1;
+  bool page_there = false;
+  const uint8_t* page_src = p.pool;
   // selected: the indices of the unit after the next one, the page numbers of the next one
   Cursor<D, NT, kTopk> idx_at = at;   // unit whose indices are loaded next
   long long idx_loaded = lo;
@@ -338,13 +379,18 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
     load_indices();
   }
 
+  unsigned seen_of[S::kStages];  // which keys of the stages under way are there at all, the oldest stage's first
+#pragma unroll
+  for (int i = 0; i < S::kStages; ++i) seen_of[i] = 0;
   auto fetch = [&]() {
+#pragma unroll
+    for (int i = 0; i + 1 < S::kStages; ++i) seen_of[i] = seen_of[i + 1];
     if (fetched < hi) {
       const uint32_t dst = ring_addr + fetch_stage * S::kUnitBytes;
       if constexpr (kTopk) {
         const bool sees = near_page >= 0 && near_page < p.pool_pages;
         const unsigned seen = __ballot_sync(0xffffffffu, sees);
-        if (lane == 0) s_seen[warp][fetch_stage] = seen;
+        seen_of[S::kStages - 1] = seen;
         const int slot = sees ? near_page * kPageKeys + near_pos % kPageKeys : -1;
         const uint8_t* head = p.pool + static_cast<long long>(ahead.kvh) * kPageKeys * S::kRow;
         constexpr int kPiece = S::kRow % 16 == 0 ? 16 : 8, kPieces = S::kRow / kPiece;
@@ -359,22 +405,23 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         step_pages();
         load_indices();
       } else {
-        const int page_no = ahead.unit / 2;
-        if (ahead.unit == 0 || pages_at < 0 || page_no - pages_at >= 32) {
-          pages_at = page_no;
-          pages = page_no + lane < p.max_pages ? p.page_table[static_cast<long long>(ahead.b) * p.max_pages + page_no + lane] : -1;
-        }
-        const int page = __shfl_sync(0xffffffffu, pages, page_no - pages_at);
-        const bool sees = page >= 0 && page < p.pool_pages;
-        if (lane == 0) s_seen[warp][fetch_stage] = sees ? 0xffffffffu : 0u;
-        if (sees) {
-          const uint8_t* src = p.pool + page * page_bytes + (static_cast<long long>(ahead.kvh) * kPageKeys + (ahead.unit & 1) * kUnit) * S::kRow;
-#pragma unroll
-          for (int i = 0; i < (S::kUnitBytes / 16 + 31) / 32; ++i) {
-            const int n = i * 32 + lane;
-            if (S::kUnitBytes / 16 % 32 == 0 || n < S::kUnitBytes / 16) cp_async<16>(dst + n * 16, src + n * 16);
+        if ((ahead.unit & 1) == 0 || fetched == lo) {  // a page, or the half that the run begins with
+          const int page_no = ahead.unit >> 1;
+          if (ahead.unit < 2 || pages_at < 0 || page_no - pages_at >= 32) {
+            pages_at = page_no;
+            pages = page_no + lane < p.max_pages ? p.page_table[static_cast<long long>(ahead.b) * p.max_pages + page_no + lane] : -1;
           }
+          const int page = __shfl_sync(0xffffffffu, pages, page_no - pages_at);
+          page_there = page >= 0 && page < p.pool_pages;
+          page_src = p.pool + (page_there ? page : 0) * page_bytes + (ahead.kvh * kPageKeys + (ahead.unit & 1) * kUnit) * S::kRow + lane * 16;
         }
+        seen_of[S::kStages - 1] = page_there ? 0xffffffffu : 0u;
+        if (page_there) {
+#pragma unroll
+          for (int i = 0; i < (S::kUnitBytes / 16 + 31) / 32; ++i)
+            if (S::kUnitBytes / 16 % 32 == 0 || i * 32 + lane < S::kUnitBytes / 16) cp_async<16>(dst + lane * 16 + i * 512, page_src + i * 512);
+        }
+        page_src += S::kUnitBytes;
       }
       ++fetched;
       if (fetched < hi) ahead.next(p, true);
@@ -385,6 +432,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
 #pragma unroll
   for (int i = 0; i < S::kStages - 1; ++i) fetch();
 
+  // (a scale of zero is taken as a tiny one, so that what is masked stays at -inf; a negative one turns the queries' signs)
+  const float to_log2 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);
   // ---- the run ----------------------------------------------------------------------------------
   if (lane < 2) s_part[warp][lane] = PartDesc{0, 0, 0, 0};
   int stage = 0;
@@ -395,9 +444,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
     const int first = kTopk ? at.b : at.w.r.first;
     const int rows = kTopk ? p.group : at.w.r.n * p.group;
     const int row0 = at.rt * S::kRows;
-    // queries as the column operand, and -24 sum q of each group of 32
+    // queries as the column operand, what the accumulators begin with, and what a column's scores are worth
     uint32_t bq[NT][S::kGroups][2][2];
-    float off[NT][S::kGroups][2];
+    float off[NT][S::kGroups][4], worth[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = row0 + nt * 8 + g;
@@ -411,22 +460,43 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
 #pragma unroll
         for (int gi = 0; gi < S::kGroups; ++gi) x[gi] = __ldg(src + gi * 4 + t);
       }
+      // the row's largest exponent; its largest element comes to lie in [2^15, 2^16), under 65,280
+      uint32_t top = 0;
 #pragma unroll
       for (int gi = 0; gi < S::kGroups; ++gi) {
-        // elements i and i + 4 of the word side by side, as the codes come
-        bq[nt][gi][0][0] = __byte_perm(x[gi].x, x[gi].z, 0x5410);
-        bq[nt][gi][0][1] = __byte_perm(x[gi].x, x[gi].z, 0x7632);
-        bq[nt][gi][1][0] = __byte_perm(x[gi].y, x[gi].w, 0x5410);
-        bq[nt][gi][1][1] = __byte_perm(x[gi].y, x[gi].w, 0x7632);
         const uint32_t w[4] = {x[gi].x, x[gi].y, x[gi].z, x[gi].w};
-        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += __uint_as_float(w[i] << 16) + __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+      }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int e = max(static_cast<int>(top >> 7), 21);  // biased exponent; rows under 2^-106 stay smaller
+      const float up = copysignf(__uint_as_float(static_cast<uint32_t>(127 + 127 + 15 - e) << 23), p.scale);
+      const float down = __uint_as_float(static_cast<uint32_t>(e - 15) << 23) * to_log2;
+#pragma unroll
+      for (int gi = 0; gi < S::kGroups; ++gi) {
+        const uint32_t w[4] = {x[gi].x, x[gi].y, x[gi].z, x[gi].w};
+        float f[8], low = 0.f, high = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f[2 * i] = __uint_as_float(w[i] << 16) * up;
+          f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u) * (up * 0.0625f);
+          low += f[2 * i];
+          high += f[2 * i + 1];
+        }
+        // elements i and i + 4 of the word side by side, as the codes come
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bq[nt][gi][i >> 1][i & 1] = half2_bits(f[i], f[i + 4]);
+        float sum = -8.f / 16777216.f * __fmaf_rn(16.f, high, low);
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        off[nt][gi][0] = -24.f * __shfl_sync(0xffffffffu, sum, 8 * t);
-        off[nt][gi][1] = -24.f * __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+        off[nt][gi][0] = off[nt][gi][2] = __shfl_sync(0xffffffffu, sum, 8 * t);
+        off[nt][gi][1] = off[nt][gi][3] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
       }
+      // (scores beyond 2^100 only have to stay finite: one key then has all the weight)
+      const float w = fminf(down * 16777216.f, 0x1p100f);
+      worth[nt][0] = __shfl_sync(0xffffffffu, w, 8 * t);
+      worth[nt][1] = __shfl_sync(0xffffffffu, w, 8 * t + 4);
     }
     // how far each column sees (dense form)
     int limit[NT][2], least = 0x7fffffff, most = -1;
@@ -451,26 +521,19 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
 #pragma unroll
         for (int c = 0; c < 4; ++c) o[j][nt][c] = 0.f;
     }
-    const float to_log2 = p.scale * kLog2e;
 
-    for (int unit = unit0; unit < unit1; ++unit, ++u) {
-      cp_wait<S::kStages - 2>();
-      __syncwarp();  // this unit has come, for all lanes, and all are through with the one before, whose stage is filled again
-      fetch();
-      const uint8_t* st = ring + stage * S::kUnitBytes;
-      const unsigned seen = s_seen[warp][stage];
-      const bool whole = seen == 0xffffffffu && (kTopk || unit * kUnit + kUnit - 1 <= least);
+    // one unit; kWhole: every row of the tile sees all its keys
+    auto take = [&](const uint8_t* st, int unit, unsigned seen, auto whole_unit) {
+      constexpr bool kWhole = decltype(whole_unit)::value;
       float y[2][NT][4];
 #pragma unroll
       for (int blk = 0; blk < 2; ++blk) {
         const uint8_t* k0 = st + (blk * 16 + g) * S::kRow;
         const uint8_t* k1 = k0 + 8 * S::kRow;
-        __half ks0[S::kGroups], ks1[S::kGroups];
-#pragma unroll
-        for (int gi = 0; gi < S::kGroups; gi += 2) {
-          *reinterpret_cast<uint32_t*>(&ks0[gi]) = *reinterpret_cast<const uint32_t*>(k0 + D + gi * 2);
-          *reinterpret_cast<uint32_t*>(&ks1[gi]) = *reinterpret_cast<const uint32_t*>(k1 + D + gi * 2);
-        }
+        struct alignas(D / 16) Scales {
+          __half s[S::kGroups];
+        };
+        const Scales ks0 = *reinterpret_cast<const Scales*>(k0 + D), ks1 = *reinterpret_cast<const Scales*>(k1 + D);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -479,14 +542,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         for (int gi = 0; gi < S::kGroups; ++gi) {
           const uint32_t w0 = *reinterpret_cast<const uint32_t*>(k0 + gi * 16 + t * 4);
           const uint32_t w1 = *reinterpret_cast<const uint32_t*>(k1 + gi * 16 + t * 4);
-          const uint32_t a00 = bf16_codes<0>(w0), a01 = bf16_codes<0>(w1), a02 = bf16_codes<1>(w0), a03 = bf16_codes<1>(w1);
-          const uint32_t a10 = bf16_codes<2>(w0), a11 = bf16_codes<2>(w1), a12 = bf16_codes<3>(w0), a13 = bf16_codes<3>(w1);
-          const float s0 = __half2float(ks0[gi]) * to_log2, s1 = __half2float(ks1[gi]) * to_log2;
+          const uint32_t x0 = w0 >> 8, x1 = w1 >> 8;
+          const float s0 = __half2float(ks0.s[gi]), s1 = __half2float(ks1.s[gi]);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            float acc[4] = {off[nt][gi][0], off[nt][gi][1], off[nt][gi][0], off[nt][gi][1]};
-            mma_bf16(acc, a00, a01, a02, a03, bq[nt][gi][0][0], bq[nt][gi][0][1]);
-            mma_bf16(acc, a10, a11, a12, a13, bq[nt][gi][1][0], bq[nt][gi][1][1]);
+            float acc[4];
+            mma_f16_from(acc, codes_low(w0), codes_low(w1), codes_high(w0), codes_high(w1), bq[nt][gi][0][0], bq[nt][gi][0][1], off[nt][gi]);
+            mma_f16(acc, codes_low(x0), codes_low(x1), codes_high(x0), codes_high(x1), bq[nt][gi][1][0], bq[nt][gi][1][1]);
             y[blk][nt][0] = __fmaf_rn(acc[0], s0, y[blk][nt][0]);
             y[blk][nt][1] = __fmaf_rn(acc[1], s0, y[blk][nt][1]);
             y[blk][nt][2] = __fmaf_rn(acc[2], s1, y[blk][nt][2]);
@@ -495,7 +557,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         }
       }
       unsigned live = seen;  // keys that some row of the tile sees: all others' values are taken as zero, whatever lies there
-      if (!whole) {
+      if constexpr (!kWhole) {
         if constexpr (!kTopk) {
           const int n = most - unit * kUnit + 1;
           live = n <= 0 ? 0u : (n >= 32 ? live : live & ((1u << n) - 1u));
@@ -531,7 +593,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-            const float back = m[nt][c] == -INFINITY ? 0.f : ex2(m[nt][c] - x);
+            const float back = m[nt][c] == -INFINITY ? 0.f : ex2(m[nt][c] * worth[nt][c] - x * worth[nt][c]);
             m[nt][c] = x;
             l[nt][c] *= back;
 #pragma unroll
@@ -544,11 +606,12 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
       uint32_t bp[2][NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0] - kPShift, m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1] - kPShift;
+        const float c0 = worth[nt][0], c1 = worth[nt][1];
+        const float m0 = m[nt][0] == -INFINITY ? 0.f : kPShift - m[nt][0] * c0, m1 = m[nt][1] == -INFINITY ? 0.f : kPShift - m[nt][1] * c1;
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
-          const float p0 = ex2(y[blk][nt][0] - m0), p1 = ex2(y[blk][nt][1] - m1);
-          const float p2 = ex2(y[blk][nt][2] - m0), p3 = ex2(y[blk][nt][3] - m1);
+          const float p0 = ex2(__fmaf_rn(y[blk][nt][0], c0, m0)), p1 = ex2(__fmaf_rn(y[blk][nt][1], c1, m1));
+          const float p2 = ex2(__fmaf_rn(y[blk][nt][2], c0, m0)), p3 = ex2(__fmaf_rn(y[blk][nt][3], c1, m1));
           l[nt][0] += p0 + p2;
           l[nt][1] += p1 + p3;
           bp[blk][nt][0] = transposed(half2_bits(p0, p1));
@@ -565,7 +628,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t a = *reinterpret_cast<const uint16_t*>(sc + h * 8 * S::kRow), b = *reinterpret_cast<const uint16_t*>(sc + (h * 8 + 1) * S::kRow);
-          if (!whole) {
+          if constexpr (!kWhole) {
             if (!((live >> (key + h * 8)) & 1u)) a = 0;
             if (!((live >> (key + h * 8 + 1)) & 1u)) b = 0;
           }
@@ -595,7 +658,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         }
         auto value = [&](int h, int x, auto e) {  // element e of word x, keys 2 t and 2 t + 1 (+ 8 h)
           constexpr int kE = decltype(e)::value;
-          return hfma2(f16_codes<kE % 4>(kE < 4 ? lo16[h][x] : hi16[h][x]), s2[h], c2[h]);
+          return f16_values<kE % 4>(kE < 4 ? lo16[h][x] : hi16[h][x], s2[h], c2[h]);
         };
         auto tile = [&](auto j) {
           constexpr int kJ = decltype(j)::value;
@@ -617,6 +680,19 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
           tile(std::integral_constant<int, 7>{});
         }
       }
+    };
+
+    for (int unit = unit0; unit < unit1; ++unit, ++u) {
+      cp_wait<S::kStages - 2>();
+      __syncwarp();  // this unit has come, for all lanes, and all are through with the one before, whose stage is filled again
+      fetch();
+      const uint8_t* st = ring + stage * S::kUnitBytes;
+      const unsigned seen = seen_of[0];
+      const bool whole = seen == 0xffffffffu && (kTopk || unit * kUnit + kUnit - 1 <= least);
+      if (whole)
+        take(st, unit, seen, std::true_type{});
+      else
+        take(st, unit, seen, std::false_type{});
       stage = stage + 1 == S::kStages ? 0 : stage + 1;
     }
 
@@ -628,6 +704,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 4);
         l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 8);
         l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 16);
+        m[nt][c] *= worth[nt][c];
       }
     const int flags = kValid | (unit0 == 0 ? kBegins : 0) | (unit1 == at.w.units ? kEnds : 0);
     const bool complete = flags == (kValid | kBegins | kEnds), last_segment = u >= hi;
@@ -673,53 +750,48 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
 
   // ---- parts of the CTA's warps, joined in the order of their units ------------------------------
   __syncthreads();
+  const int my_flags = lane < 2 * S::kWarps ? s_part[lane >> 1][lane & 1].flags : 0;
+  const unsigned parts = __ballot_sync(0xffffffffu, my_flags & kValid), begin_at = __ballot_sync(0xffffffffu, my_flags & kBegins),
+                 end_at = __ballot_sync(0xffffffffu, my_flags & kEnds);
+  static_assert(2 * S::kWarps <= 32, "a bit for every part");
   CtaDesc* desc = sb.desc + blockIdx.x;
   if (tid < 2) {
-    // which items are left open: the first part's if it does not begin here, the last one's if it does not end
+    // the items that are left open: the one that the first part goes on with if it does not begin here, and the one that the last part
+    // belongs to if that item begins here and does not end
     PartDesc open{0, 0, 0, 0};
-    PartDesc run{0, 0, 0, 0};
-    for (int i = 0; i < 2 * S::kWarps; ++i) {
-      const PartDesc d = s_part[i >> 1][i & 1];
-      if (!(d.flags & kValid)) continue;
-      const bool same = (run.flags & kValid) && !(run.flags & kEnds) && d.b == run.b && d.kvh == run.kvh && d.rt == run.rt;
-      if (same) run.flags |= d.flags & kEnds; else run = d;
-      const bool begins = run.flags & kBegins, ends = run.flags & kEnds;
-      if (tid == 0 ? !begins : (begins && !ends)) open = run;
-      if (tid == 1 && begins && ends) open.flags = 0;
+    const int first_part = __ffs(parts) - 1, last_begin = 31 - __clz(begin_at | 1u);
+    if (tid == 0 && parts != 0 && !((begin_at >> first_part) & 1u)) {
+      open = s_part[first_part >> 1][first_part & 1];
+      const unsigned its = begin_at != 0 ? (1u << (__ffs(begin_at) - 1)) - 1u : 0xffffffffu;  // parts before any other item begins
+      open.flags |= (end_at & its) != 0 ? kEnds : 0;
     }
+    if (tid == 1 && begin_at != 0 && (end_at >> last_begin) == 0) open = s_part[last_begin >> 1][last_begin & 1];
     desc->part[tid] = open;
   }
+  if (parts == 0) return;
   for (int v = tid; v < S::kRows * D / 4; v += S::kThreads) {
     const int n = v * 4 / D, d = v * 4 % D;
-    PartDesc run{0, 0, 0, 0};
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < 2 * S::kWarps; ++i) {
-      const PartDesc pd = s_part[i >> 1][i & 1];
-      if (!(pd.flags & kValid)) continue;
-      if (pd.flags & kBegins || !(run.flags & kValid)) {
-        run = pd;
-        o = make_float4(0.f, 0.f, 0.f, 0.f);
-        m = -INFINITY;
-        l = 0.f;
-      } else {
-        run.flags |= pd.flags & kEnds;
-      }
+    bool begins = false;
+    for (unsigned left = parts; left != 0; left &= left - 1) {
+      const int i = __ffs(left) - 1;
       const float* part = i & 1 ? reinterpret_cast<const float*>(smem + static_cast<size_t>(i >> 1) * S::kRingBytes)
                                 : sb.warp + (static_cast<long long>(blockIdx.x) * S::kWarps + (i >> 1)) * S::kPartFloats;
       const float4 x = *reinterpret_cast<const float4*>(part + n * D + d);
       const float pm = part[S::kRows * D + n], pl = part[S::kRows * D + S::kRows + n];
-      const float mm = fmaxf(m, pm), a = m == -INFINITY ? 0.f : ex2(m - mm), b = pm == -INFINITY ? 0.f : ex2(pm - mm);
-      o = make_float4(o.x * a + x.x * b, o.y * a + x.y * b, o.z * a + x.z * b, o.w * a + x.w * b);
-      l = l * a + pl * b;
-      m = mm;
-      const bool begins = run.flags & kBegins, ends = run.flags & kEnds;
-      // does the item go on in a later part of this CTA?
-      bool more = false;
-      if (!ends)
-        for (int k = i + 1; k < 2 * S::kWarps && !more; ++k) more = s_part[k >> 1][k & 1].flags & kValid;
-      if (more) continue;
+      if ((begin_at >> i) & 1u) {
+        begins = true;
+        o = x;
+        m = pm;
+        l = pl;
+      } else {
+        join(o, m, l, x, pm, pl);
+      }
+      const bool ends = (end_at >> i) & 1u;
+      if (!ends && (left & (left - 1)) != 0) continue;  // the item goes on in the next part
       if (begins && ends) {
+        const PartDesc run = s_part[i >> 1][i & 1];
         int first = run.b, rows = p.group;
         if constexpr (!kTopk) {
           const Kv4Request r = kv4_request(p, run.b);
@@ -740,7 +812,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
           to[S::kRows * D + S::kRows + n] = l;
         }
       }
-      run.flags = 0;
+      o = make_float4(0.f, 0.f, 0.f, 0.f);
+      m = -INFINITY;
+      l = 0.f;
+      begins = false;
     }
   }
 }
@@ -752,6 +827,23 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Kv4AttnParams
   chain_wait();
   const PartDesc run = sb.desc[blockIdx.x].part[1];
   if (!(run.flags & kValid)) return;
+  // the CTAs behind this one that hold pieces of it: up to the first whose piece ends it
+  int n_more = 0;
+  for (int base = blockIdx.x + 1; base < n_ctas; base += 256) {
+    const int c = base + threadIdx.x;
+    const int flags = c < n_ctas ? sb.desc[c].part[0].flags : 0;
+    const bool ends = (flags & kEnds) != 0;
+    // (a run without units has no piece, and takes no part in the order)
+    __shared__ int s_end;
+    if (threadIdx.x == 0) s_end = n_ctas;
+    __syncthreads();
+    if (ends) atomicMin(&s_end, c);
+    __syncthreads();
+    n_more = (s_end < n_ctas ? s_end + 1 : n_ctas) - (blockIdx.x + 1);
+    const bool found = s_end < n_ctas;
+    __syncthreads();
+    if (found) break;
+  }
   int first = run.b, rows = p.group;
   if constexpr (!kTopk) {
     const Kv4Request r = kv4_request(p, run.b);
@@ -764,17 +856,25 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Kv4AttnParams
     const float* part = sb.cta + (static_cast<long long>(blockIdx.x) * 2 + 1) * S::kPartFloats;
     float4 o = *reinterpret_cast<const float4*>(part + n * D + d);
     float m = part[S::kRows * D + n], l = part[S::kRows * D + S::kRows + n];
-    for (int c = blockIdx.x + 1; c < n_ctas; ++c) {
-      const int flags = sb.desc[c].part[0].flags;
-      if (!(flags & kValid)) continue;  // (a run without units)
-      part = sb.cta + static_cast<long long>(c) * 2 * S::kPartFloats;
-      const float4 x = *reinterpret_cast<const float4*>(part + n * D + d);
-      const float pm = part[S::kRows * D + n], pl = part[S::kRows * D + S::kRows + n];
-      const float mm = fmaxf(m, pm), a = m == -INFINITY ? 0.f : ex2(m - mm), b = pm == -INFINITY ? 0.f : ex2(pm - mm);
-      o = make_float4(o.x * a + x.x * b, o.y * a + x.y * b, o.z * a + x.z * b, o.w * a + x.w * b);
-      l = l * a + pl * b;
-      m = mm;
-      if (flags & kEnds) break;
+    constexpr int kAhead = 8;  // pieces under way at once
+    for (int c0 = 0; c0 < n_more; c0 += kAhead) {
+      float4 x[kAhead];
+      float pm[kAhead], pl[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        pm[i] = -INFINITY;
+        pl[i] = 0.f;
+        const int c = blockIdx.x + 1 + c0 + i;
+        if (c0 + i < n_more && (sb.desc[c].part[0].flags & kValid)) {
+          part = sb.cta + static_cast<long long>(c) * 2 * S::kPartFloats;
+          x[i] = *reinterpret_cast<const float4*>(part + n * D + d);
+          pm[i] = part[S::kRows * D + n];
+          pl[i] = part[S::kRows * D + S::kRows + n];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) join(o, m, l, x[i], pm[i], pl[i]);
     }
     int token, head;
     row_place(p, first, run.kvh, r, token, head);
