@@ -14,7 +14,7 @@
 //     half of them need no shift.  Queries are scaled by a power of two to fp16's range (exact but for what is under 2^-35 of the row's
 //     largest), those that meet u 2^-20 by a further 1 / 16; the accumulators start at -8 sum q, so that they end at sum q (u - 8),
 //     exact products in fp32, and the scale of (key, group) multiplies that in fp32.
-//   P^T: the accumulators, in fp16, turned by movmatrix.  p is held times 2^15, so that fp16 reaches down to 2^-39 of the largest.
+//   P^T: the accumulators, in fp16, turned by movmatrix.
 //   O^T = V^T P^T: lane (g, t) holds elements 16 g .. 16 g + 15 of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9: one scale group, words that pair up
 //     by two byte permutations.  A value is (16 + u) s - 24 s, one FMA on fp16 pairs, for the nibbles that are shifted there anyway; for
 //     the others (1024 + u) - 1032 or (1024 + 16 u) / 16 - 72, exact, times s: an FMA more and a shift less, which evens out the pipes.
@@ -37,7 +37,11 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 #define KW2 8
 #define KST 3
 #endif
-constexpr float kPShift = 15.f;    // probabilities are held times 2^15
+// Probabilities are held times 2^11, relative to a maximum that is only raised when a score has passed it by 4 powers of two (raising
+// it multiplies all sums, and for 8 heads some score passes the exact maximum in every third unit): at most 2^15, and no less
+// than 2^-35 of the largest in fp16.
+constexpr float kPShift = 11.f, kPSlack = 4.f;
+constexpr float kNothing = 1e30f;  // shift of a row that has seen nothing
 
 template <int D, int NT>
 struct Shape {
@@ -119,12 +123,30 @@ __device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
   asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
+// A constant that stays in a register: instructions take one immediate, and the ones below would need two.
+__device__ __forceinline__ uint32_t held(uint32_t x) {
+  uint32_t r;
+  asm("mov.b32 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+struct ValueConstants {
+  uint32_t k1024, k16, inv16, minus72;
+  __device__ __forceinline__ ValueConstants() : k1024(held(0x64006400u)), k16(held(0x4C004C00u)), inv16(held(0x2C002C00u)), minus72(held(0xD480D480u)) {}
+};
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t c) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "r"(mask), "r"(c));
+  return d;
+}
 // Nibble i of each half of w as the fp16 pair (u - 8) s, rounded once; minus24s = -24 s.
 template <int i>
-__device__ __forceinline__ uint32_t f16_values(uint32_t w, uint32_t s, uint32_t minus24s) {
-  if constexpr (i == 0) return hmul2(hadd2(codes_low(w) | 0x64006400u, 0xE408E408u), s);                // - 1032
-  if constexpr (i == 1) return hmul2(hfma2(codes_high(w) | 0x64006400u, 0x2C002C00u, 0xD480D480u), s);  // / 16 - 72
-  return hfma2(((w >> (4 * i - 6)) & 0x03C003C0u) | 0x4C004C00u, s, minus24s);               // 16 + u
+__device__ __forceinline__ uint32_t f16_values(uint32_t w, uint32_t s, uint32_t minus24s, const ValueConstants& k) {
+  if constexpr (i == 0)
+    return hmul2(hadd2(and_or(w, 0x000F000Fu, k.k1024), 0xE408E408u), s);  // 1024 + u - 1032
+  else if constexpr (i == 1)
+    return hmul2(hfma2(and_or(w, 0x00F000F0u, k.k1024), k.inv16, k.minus72), s);  // (1024 + 16 u) / 16 - 72
+  else
+    return hfma2(and_or(w >> (4 * i - 6), 0x03C003C0u, k.k16), s, minus24s);  // 16 + u
 }
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -511,10 +533,12 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
       least = at.w.r.ctx + row0 / p.group;
       most = at.w.r.ctx + ((row0 + S::kRows < rows ? row0 + S::kRows : rows) - 1) / p.group;
     }
-    float o[S::kTilesD][NT][4], m[NT][2], l[NT][2];
+    float o[S::kTilesD][NT][4], l[NT][2];
+    float bar[NT][2], shift[NT][2];  // scores beyond bar raise the maximum m; shift = kPShift - m, in powers of two
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = -INFINITY;
+      bar[nt][0] = bar[nt][1] = -INFINITY;
+      shift[nt][0] = shift[nt][1] = kNothing;
       l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
       for (int j = 0; j < S::kTilesD; ++j)
@@ -522,6 +546,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         for (int c = 0; c < 4; ++c) o[j][nt][c] = 0.f;
     }
 
+    const ValueConstants constants;
     // one unit; kWhole: every row of the tile sees all its keys
     auto take = [&](const uint8_t* st, int unit, unsigned seen, auto whole_unit) {
       constexpr bool kWhole = decltype(whole_unit)::value;
@@ -574,7 +599,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
               if (!ok) y[blk][nt][c] = -INFINITY;
             }
       }
-      // the running maximum, only where some lane has a larger one
       bool grows = false;
       float top[NT][2];
 #pragma unroll
@@ -582,32 +606,34 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           top[nt][c] = fmaxf(fmaxf(y[0][nt][c], y[0][nt][c + 2]), fmaxf(y[1][nt][c], y[1][nt][c + 2]));
-          grows = grows || top[nt][c] > m[nt][c];
+          grows = grows || top[nt][c] > bar[nt][c];
         }
       if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float x = fmaxf(top[nt][c], m[nt][c]);
+            float x = top[nt][c];
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-            const float back = m[nt][c] == -INFINITY ? 0.f : ex2(m[nt][c] * worth[nt][c] - x * worth[nt][c]);
-            m[nt][c] = x;
-            l[nt][c] *= back;
+            if (x > bar[nt][c]) {  // (the same in all lanes of the column)
+              const float now = kPShift - x * worth[nt][c], back = ex2(now - shift[nt][c]);
+              bar[nt][c] = x + kPSlack / worth[nt][c];
+              shift[nt][c] = now;
+              l[nt][c] *= back;
 #pragma unroll
-            for (int j = 0; j < S::kTilesD; ++j) {
-              o[j][nt][c] *= back;
-              o[j][nt][c + 2] *= back;
+              for (int j = 0; j < S::kTilesD; ++j) {
+                o[j][nt][c] *= back;
+                o[j][nt][c + 2] *= back;
+              }
             }
           }
       }
       uint32_t bp[2][NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float c0 = worth[nt][0], c1 = worth[nt][1];
-        const float m0 = m[nt][0] == -INFINITY ? 0.f : kPShift - m[nt][0] * c0, m1 = m[nt][1] == -INFINITY ? 0.f : kPShift - m[nt][1] * c1;
+        const float c0 = worth[nt][0], c1 = worth[nt][1], m0 = shift[nt][0], m1 = shift[nt][1];
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
           const float p0 = ex2(__fmaf_rn(y[blk][nt][0], c0, m0)), p1 = ex2(__fmaf_rn(y[blk][nt][1], c1, m1));
@@ -658,7 +684,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         }
         auto value = [&](int h, int x, auto e) {  // element e of word x, keys 2 t and 2 t + 1 (+ 8 h)
           constexpr int kE = decltype(e)::value;
-          return f16_values<kE % 4>(kE < 4 ? lo16[h][x] : hi16[h][x], s2[h], c2[h]);
+          return f16_values<kE % 4>(kE < 4 ? lo16[h][x] : hi16[h][x], s2[h], c2[h], constants);
         };
         auto tile = [&](auto j) {
           constexpr int kJ = decltype(j)::value;
@@ -697,6 +723,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
     }
 
     // ---- the item's end, or the run's -----------------------------------------------------------
+    float m[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -704,7 +731,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 4);
         l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 8);
         l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 16);
-        m[nt][c] *= worth[nt][c];
+        m[nt][c] = l[nt][c] > 0.f ? kPShift - shift[nt][c] : -INFINITY;
       }
     const int flags = kValid | (unit0 == 0 ? kBegins : 0) | (unit1 == at.w.units ? kEnds : 0);
     const bool complete = flags == (kValid | kBegins | kEnds), last_segment = u >= hi;

@@ -96,15 +96,16 @@ class Step:
     def check(self, out, lse, idx=None, fused=True, n_most=None):
         """Against the 64-bit definition, within what the roundings on the way can do.
 
-        Fused path.  A score is a sum of exact products accumulated in fp32 over codes offset by 24 (16 + u, taken from
-        -24 sum q): no more than 64 |q_d| s per element pass through an accumulator, in at most 4 roundings of 2^-22 each; the tiled
+        Fused path.  A score is a sum of exact products accumulated in fp32 over codes offset by 8 (u, begun at -8 sum q):
+        no more than 64 |q_d| s per element pass through an accumulator, in at most 4 roundings of 2^-22 each; the tiled
         form instead rounds key values, of 12 significant bits, to fp16 (2^-11 of scale * sum |q k|).  So a score is off by
         at most ds = weight * (2^-11 + 64 * 4 * 2^-22) where weight >= scale * sum |q k|; |code| >= 1 for most elements but not
         for all, which the factor 4 on the second term covers.  A probability is then off by the factor e^ds, by 2^-11 for its
         rounding to fp16, and the value by 2^-11 for its own; numerator and denominator both move: 2 ds + 2 * 2^-11, with 2^-20
-        for sums and exponentials, of spread = sum p |v|.  Probabilities under 2^-29 of the largest are subnormal in
-        fp16, times 2^15 as they are held: their rounding is not relative but up to 2^-25, so 2^-40 of the largest each, which shows in an
-        element whose code is 0 at every key that matters (2^-40 mass, mass = sum |v|; the largest probability is at most the sum).
+        for sums and exponentials, of spread = sum p |v|.  Small probabilities are subnormal in
+        fp16, times 2^11 as they are held relative to a maximum that is at most the largest: their rounding is not relative but up to
+        2^-25, so 2^-36 of the largest each, which shows in an element whose code is 0 at every key that matters (2^-36 mass,
+        mass = sum |v|; the largest probability is at most the sum).
         The result is rounded to bf16 (2^-8 of itself).
         fp32 path: ds = weight * (D + 8) 2^-24, sums of n terms, and a result rounded to 2^-24."""
         ref, ref_lse, spread, weight, mass = kv4.attention(self.q, self.pool, self.table, self.start, self.ctx, self.scale, idx)
@@ -112,7 +113,7 @@ class Step:
         assert np.array_equal(out[end:], np.full_like(out[end:], 7.0)), "rows behind the last request were written"
         if fused:
             ds = weight * (2.0**-11 + 4 * 256 * 2.0**-22)
-            rel, last, sums, lost = 2 * ds + 2 * 2.0**-11 + 2.0**-20, 2.0**-8, 2.0**-20, 2.0**-40
+            rel, last, sums, lost = 2 * ds + 2 * 2.0**-11 + 2.0**-20, 2.0**-8, 2.0**-20, 2.0**-36
         else:
             n = n_most or int((self.ctx + self.new).max())
             ds = weight * (self.D + 8) * 2.0**-24
