@@ -847,6 +847,9 @@ int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t
   return LT_OK;
 }
 
+// Rows of a request (or token) up to which the few-row kernel takes it, and from which the tiled kernel takes pairs of tiles.
+static constexpr int kKv4FewRows = 32, kKv4FewRowsTopk = 16, kKv4PairRows = 256;
+
 static int kv4_attention_impl(int dtype, const void* q, long long q_stride, const void* pool, long long pool_pages,
                               const int32_t* page_table, int max_pages, const int32_t* query_start, const int32_t* context_len,
                               const int32_t* idx, int topk, int B, int T, int Hq, int Hkv, int D, int max_new, float scale,
@@ -885,15 +888,31 @@ static int kv4_attention_impl(int dtype, const void* q, long long q_stride, cons
   p.lse = lse;
   p.min_rows = 1;
   p.max_rows = INT_MAX;
+  p.ctl = static_cast<Control*>(workspace);
+  p.wait_limit_us = tun.wait_limit_us > 0 ? tun.wait_limit_us : 2000000u;
   if (dtype == LT_DTYPE_F32 || tun.path == LT_PATH_GENERIC) {
     LT_LAUNCH(launch_kv4_attention_generic(dtype, D, p, stream));
     return LT_OK;
   }
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
-  const long long tokens = idx != nullptr ? 1 : (max_new > 0 && max_new < T ? max_new : T);  // most of any request
+  // few rows (tokens x heads of a group) go to one kernel, many to the other; requests of both kinds share a batch
+  uint8_t* scratch = static_cast<uint8_t*>(workspace) + kAlign;
   const int sms = sm_count(), grid = tun.grid > 0 && tun.grid < sms ? tun.grid : sms;
-  LT_LAUNCH(launch_kv4_attention_rows(D, tokens * p.group, p, ws, grid, stream));
-  ++g_launches;  // (two kernels)
+  const long long tokens = idx != nullptr ? 1 : (max_new > 0 && max_new < T ? max_new : T);  // most of any request
+  const long long most_rows = tokens * p.group;
+  const int few = idx != nullptr ? kKv4FewRowsTopk : kKv4FewRows;
+  bool launched = false;
+  if (idx == nullptr || most_rows <= few) {
+    p.max_rows = few;
+    LT_LAUNCH(launch_kv4_attention_rows(D, most_rows < few ? most_rows : few, p, scratch, p.ctl, grid, stream));
+    ++g_launches;  // (two kernels)
+    launched = true;
+  }
+  if (most_rows > few) {
+    p.min_rows = few + 1;
+    p.max_rows = INT_MAX;
+    LT_LAUNCH(launch_kv4_attention_tiles(D, most_rows >= kKv4PairRows, p, scratch, p.ctl, grid, launched, stream));
+    ++g_launches;
+  }
   return LT_OK;
 }
 
@@ -916,7 +935,9 @@ int lt_kv4_attention_topk(int dtype, const void* q, long long q_stride, const vo
 
 size_t lt_kv4_attention_workspace_bytes(int dtype, int T, int B, int Hq, int Hkv, int D) {
   if (!kv4_dtype(dtype) || !kv4_shape(Hkv, D) || T <= 0 || B <= 0 || Hq <= 0 || Hq % Hkv != 0) return 0;
-  return dtype == LT_DTYPE_BF16 ? align_up(kv4_rows_scratch_bytes(D)) : kAlign;
+  if (dtype == LT_DTYPE_F32) return kAlign;
+  const size_t rows = kv4_rows_scratch_bytes(D), tiles = kv4_tiles_scratch_bytes(D);
+  return kAlign + align_up(rows > tiles ? rows : tiles);
 }
 
 int lt_indexer_sample_plan(int N, int topk, int causal_offset, const lt_tunables* tunables, int plan3[3]) {

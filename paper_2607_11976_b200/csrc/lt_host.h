@@ -310,7 +310,13 @@ struct Kv4AttnParams;
 // lt_kv4_attention.cu: bf16 queries, few rows (tokens x heads of a group, at most most_rows for any request or token).  scratch:
 // kv4_rows_scratch_bytes(D) bytes for up to sm_count() CTAs.
 size_t kv4_rows_scratch_bytes(int D);
-cudaError_t launch_kv4_attention_rows(int D, long long most_rows, const Kv4AttnParams& p, void* scratch, int grid, cudaStream_t stream);
+cudaError_t launch_kv4_attention_rows(int D, long long most_rows, const Kv4AttnParams& p, void* scratch, Control* ctl, int grid,
+                                      cudaStream_t stream);
+// lt_kv4_tiles.cu: bf16 queries, many rows.  pairs: 256 rows per CTA, else 128 (always, for an indexer's positions).  keep_status: the
+// call's status block already holds bits of an earlier launch.  scratch: kv4_tiles_scratch_bytes(D).
+size_t kv4_tiles_scratch_bytes(int D);
+cudaError_t launch_kv4_attention_tiles(int D, bool pairs, const Kv4AttnParams& p, void* scratch, Control* ctl, int sms, bool keep_status,
+                                       cudaStream_t stream);
 // lt_kv4_generic.cu
 // One CTA per (token, query head), any head count, fp32 arithmetic throughout.
 cudaError_t launch_kv4_attention_generic(int dtype, int D, const Kv4AttnParams& p, cudaStream_t stream);

@@ -67,6 +67,8 @@ struct Kv4AttnParams {
   float scale;
   void* out;                 // [T][Hq][D]
   float* lse;                // [T][Hq] or null
+  Control* ctl;              // the call's status block
+  unsigned int wait_limit_us;  // bound of every device-side wait
   int min_rows, max_rows;    // requests with min_rows .. max_rows (token, head of the group) rows are this kernel's
 };
 

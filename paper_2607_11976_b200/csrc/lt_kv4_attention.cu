@@ -23,25 +23,12 @@
 // runs, one per warp, whatever the lengths.  A warp has its own ring of cp.async stages and waits for nobody.  Items that it
 // sees whole it writes out itself; the parts of others are joined first within the CTA, then, where an item spans CTAs, by a
 // second kernel.  Runs are a matter of the lengths alone, so results do not vary.
-#include <type_traits>
-
-#include "lt_kv4.cuh"
+#include "lt_kv4_parts.cuh"
 
 namespace lt {
 namespace {
 
 constexpr int kUnit = 32;          // keys of a unit
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-#ifndef KW1
-#define KW1 12
-#define KW2 8
-#define KST 3
-#endif
-// Probabilities are held times 2^11, relative to a maximum that is only raised when a score has passed it by 4 powers of two (raising
-// it multiplies all sums, and for 8 heads some score passes the exact maximum in every third unit): at most 2^15, and no less
-// than 2^-35 of the largest in fp16.
-constexpr float kPShift = 11.f, kPSlack = 4.f;
-constexpr float kNothing = 1e30f;  // shift of a row that has seen nothing
 
 template <int D, int NT>
 struct Shape {
@@ -49,32 +36,18 @@ struct Shape {
   static constexpr int kGroups = D / kKvGroup;
   static constexpr int kRows = 8 * NT;       // query rows of an item
   static constexpr int kTilesD = D / 16;     // 16-row tiles of O^T
-  static constexpr int kWarps = NT == 1 ? KW1 : KW2;
+  static constexpr int kWarps = NT == 1 ? 12 : 8;
   static constexpr int kThreads = kWarps * 32;
-  static constexpr int kStages = KST;
+  static constexpr int kStages = 3;
   static constexpr int kUnitBytes = kUnit * kRow;
-  static constexpr int kPartFloats = kRows * (D + 2);  // a part: o[kRows][D], m[kRows], l[kRows]
+  static constexpr int kPartFloats = part_floats(kRows, D);
   static constexpr int kRingBytes = kStages * kUnitBytes;
   static constexpr int kPartInRing = kPartFloats * 4 <= kRingBytes;
   static constexpr size_t kSmem = static_cast<size_t>(kWarps) * kRingBytes;
   static_assert(kPartInRing, "a warp leaves its last part in its ring");
 };
 
-// A piece of an item: which rows, and whether it holds the item's first and last unit.
-struct PartDesc {
-  int b, kvh, rt, flags;
-};
-constexpr int kValid = 1, kBegins = 2, kEnds = 4;
-struct CtaDesc {
-  PartDesc part[2];  // [0] an item that began before this CTA's run, [1] one that begins in it and does not end
-};
-
 // ---- PTX ------------------------------------------------------------------------------------
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -108,61 +81,6 @@ __device__ __forceinline__ void cp_wait() {
 // Nibbles 0 and 1 of each half of w as fp16 pairs u 2^-24 and u 2^-20; nibbles 2 and 3 are those of w >> 8.
 __device__ __forceinline__ uint32_t codes_low(uint32_t w) { return w & 0x000F000Fu; }
 __device__ __forceinline__ uint32_t codes_high(uint32_t w) { return w & 0x00F000F0u; }
-__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-// A constant that stays in a register: instructions take one immediate, and the ones below would need two.
-__device__ __forceinline__ uint32_t held(uint32_t x) {
-  uint32_t r;
-  asm("mov.b32 %0, %1;" : "=r"(r) : "r"(x));
-  return r;
-}
-struct ValueConstants {
-  uint32_t k1024, k16, inv16, minus72;
-  __device__ __forceinline__ ValueConstants() : k1024(held(0x64006400u)), k16(held(0x4C004C00u)), inv16(held(0x2C002C00u)), minus72(held(0xD480D480u)) {}
-};
-__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t c) {
-  uint32_t d;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "r"(mask), "r"(c));
-  return d;
-}
-// Nibble i of each half of w as the fp16 pair (u - 8) s, rounded once; minus24s = -24 s.
-template <int i>
-__device__ __forceinline__ uint32_t f16_values(uint32_t w, uint32_t s, uint32_t minus24s, const ValueConstants& k) {
-  if constexpr (i == 0)
-    return hmul2(hadd2(and_or(w, 0x000F000Fu, k.k1024), 0xE408E408u), s);  // 1024 + u - 1032
-  else if constexpr (i == 1)
-    return hmul2(hfma2(and_or(w, 0x00F000F0u, k.k1024), k.inv16, k.minus72), s);  // (1024 + 16 u) / 16 - 72
-  else
-    return hfma2(and_or(w >> (4 * i - 6), 0x03C003C0u, k.k16), s, minus24s);  // 16 + u
-}
-__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t bf162_bits(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-// Quotient of counts that nearly always fit into 32 bits.
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
-  return a / b;
-}
-
 // ---- items ----------------------------------------------------------------------------------
 template <int D, int NT>
 struct RequestWork {
@@ -212,61 +130,6 @@ struct Cursor {
   __device__ __forceinline__ void next(const Kv4AttnParams& p, bool more) {
     if (++unit == w.units && more) next_item(p);
   }
-};
-
-// Exclusive sum over the CTA's threads, and the total.
-template <int kWarps>
-__device__ __forceinline__ long long block_scan(long long v, long long& total, long long* warp_sums) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long inc = v;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, inc, d);
-    if (lane >= d) inc += x;
-  }
-  if (lane == 31) warp_sums[warp] = inc;
-  __syncthreads();
-  long long before = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    const long long x = warp_sums[w];
-    before += w < warp ? x : 0;
-    total += x;
-  }
-  __syncthreads();
-  return before + inc - v;
-}
-
-// Row r of an item's request (dense) or token (selected): where its query and result are.
-__device__ __forceinline__ void row_place(const Kv4AttnParams& p, int first, int kvh, int r, int& token, int& head) {
-  const int j = r / p.group;
-  token = first + j;
-  head = kvh * p.group + (r - j * p.group);
-}
-
-// 4 joined elements of a row and its sum: out, and lse once per row.
-template <int D>
-__device__ __forceinline__ void write_row4(const Kv4AttnParams& p, int token, int head, int d, const float4& o, float m, float l) {
-  const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
-  __nv_bfloat16* at = static_cast<__nv_bfloat16*>(p.out) + (static_cast<long long>(token) * p.Hq + head) * D + d;
-  *reinterpret_cast<uint2*>(at) = make_uint2(bf162_bits(o.x * inv, o.y * inv), bf162_bits(o.z * inv, o.w * inv));
-  if (d == 0 && p.lse != nullptr)
-    p.lse[static_cast<long long>(token) * p.Hq + head] = l > 0.f ? (m - kPShift + log2f(l)) * kLn2 : -INFINITY;
-}
-
-// (o, m, l) and another part of the same row: sums relative to the larger maximum.
-__device__ __forceinline__ void join(float4& o, float& m, float& l, const float4& x, float pm, float pl) {
-  const float mm = fmaxf(m, pm), a = m == -INFINITY ? 0.f : ex2(m - mm), b = pm == -INFINITY ? 0.f : ex2(pm - mm);
-  o = make_float4(o.x * a + x.x * b, o.y * a + x.y * b, o.z * a + x.z * b, o.w * a + x.w * b);
-  l = l * a + pl * b;
-  m = mm;
-}
-
-struct SplitBuffers {
-  CtaDesc* desc;   // [grid]
-  float* cta;      // [grid][2][kPartFloats]
-  float* warp;     // [grid * kWarps][kPartFloats]: the first, incomplete item of a warp that goes on to others
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -794,6 +657,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
     }
     if (tid == 1 && begin_at != 0 && (end_at >> last_begin) == 0) open = s_part[last_begin >> 1][last_begin & 1];
     desc->part[tid] = open;
+    if (tid == 0) desc->status = 0;
   }
   if (parts == 0) return;
   for (int v = tid; v < S::kRows * D / 4; v += S::kThreads) {
@@ -847,68 +711,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
   }
 }
 
-// Items that span CTAs: CTA c joins the one that begins in run c with the pieces of the runs behind it.
-template <int D, int NT, bool kTopk>
-__global__ void __launch_bounds__(256) attention_join_kernel(const Kv4AttnParams p, const SplitBuffers sb, int n_ctas) {
-  using S = Shape<D, NT>;
-  chain_wait();
-  const PartDesc run = sb.desc[blockIdx.x].part[1];
-  if (!(run.flags & kValid)) return;
-  // the CTAs behind this one that hold pieces of it: up to the first whose piece ends it
-  int n_more = 0;
-  for (int base = blockIdx.x + 1; base < n_ctas; base += 256) {
-    const int c = base + threadIdx.x;
-    const int flags = c < n_ctas ? sb.desc[c].part[0].flags : 0;
-    const bool ends = (flags & kEnds) != 0;
-    // (a run without units has no piece, and takes no part in the order)
-    __shared__ int s_end;
-    if (threadIdx.x == 0) s_end = n_ctas;
-    __syncthreads();
-    if (ends) atomicMin(&s_end, c);
-    __syncthreads();
-    n_more = (s_end < n_ctas ? s_end + 1 : n_ctas) - (blockIdx.x + 1);
-    const bool found = s_end < n_ctas;
-    __syncthreads();
-    if (found) break;
-  }
-  int first = run.b, rows = p.group;
-  if constexpr (!kTopk) {
-    const Kv4Request r = kv4_request(p, run.b);
-    first = r.first;
-    rows = r.n * p.group;
-  }
-  for (int v = blockIdx.y * 256 + threadIdx.x; v < S::kRows * D / 4; v += gridDim.y * 256) {
-    const int n = v * 4 / D, d = v * 4 % D, r = run.rt * S::kRows + n;
-    if (r >= rows) continue;
-    const float* part = sb.cta + (static_cast<long long>(blockIdx.x) * 2 + 1) * S::kPartFloats;
-    float4 o = *reinterpret_cast<const float4*>(part + n * D + d);
-    float m = part[S::kRows * D + n], l = part[S::kRows * D + S::kRows + n];
-    constexpr int kAhead = 8;  // pieces under way at once
-    for (int c0 = 0; c0 < n_more; c0 += kAhead) {
-      float4 x[kAhead];
-      float pm[kAhead], pl[kAhead];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        pm[i] = -INFINITY;
-        pl[i] = 0.f;
-        const int c = blockIdx.x + 1 + c0 + i;
-        if (c0 + i < n_more && (sb.desc[c].part[0].flags & kValid)) {
-          part = sb.cta + static_cast<long long>(c) * 2 * S::kPartFloats;
-          x[i] = *reinterpret_cast<const float4*>(part + n * D + d);
-          pm[i] = part[S::kRows * D + n];
-          pl[i] = part[S::kRows * D + S::kRows + n];
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) join(o, m, l, x[i], pm[i], pl[i]);
-    }
-    int token, head;
-    row_place(p, first, run.kvh, r, token, head);
-    write_row4<D>(p, token, head, d, o, m, l);
-  }
-}
-
 template <int D, int NT>
 size_t split_bytes(int grid) {
   using S = Shape<D, NT>;
@@ -916,7 +718,7 @@ size_t split_bytes(int grid) {
 }
 
 template <int D, int NT, bool kTopk>
-cudaError_t launch_rows(const Kv4AttnParams& p, void* scratch, int grid, cudaStream_t stream) {
+cudaError_t launch_rows(const Kv4AttnParams& p, void* scratch, Control* ctl, int grid, cudaStream_t stream) {
   using S = Shape<D, NT>;
   static std::atomic<unsigned long long> allowed{0};
   const cudaError_t e = allow_smem(reinterpret_cast<const void*>(attention_rows_kernel<D, NT, kTopk>), allowed);
@@ -925,9 +727,11 @@ cudaError_t launch_rows(const Kv4AttnParams& p, void* scratch, int grid, cudaStr
   sb.cta = static_cast<float*>(scratch);
   sb.warp = sb.cta + static_cast<size_t>(grid) * 2 * S::kPartFloats;
   sb.desc = reinterpret_cast<CtaDesc*>(sb.warp + static_cast<size_t>(grid) * S::kWarps * S::kPartFloats);
+  sb.ctl = ctl;
   const cudaError_t r = launch_chained(attention_rows_kernel<D, NT, kTopk>, dim3(grid), dim3(S::kThreads), S::kSmem, stream, 1, p, sb);
   if (r != cudaSuccess) return r;
-  return launch_chained(attention_join_kernel<D, NT, kTopk>, dim3(grid, (S::kRows * D / 4 + 255) / 256), dim3(256), 0, stream, 1, p, sb, grid);
+  return launch_chained(attention_join_kernel<D, S::kRows, kTopk>, dim3(grid, (S::kRows * D / 4 + 255) / 256), dim3(256), 0, stream, 1, p,
+                        sb, grid, false);
 }
 
 }  // namespace
@@ -939,14 +743,15 @@ size_t kv4_rows_scratch_bytes(int D) {
   return a > b ? a : b;
 }
 
-cudaError_t launch_kv4_attention_rows(int D, long long most_rows, const Kv4AttnParams& p, void* scratch, int grid, cudaStream_t stream) {
+cudaError_t launch_kv4_attention_rows(int D, long long most_rows, const Kv4AttnParams& p, void* scratch, Control* ctl, int grid,
+                                      cudaStream_t stream) {
   const bool wide = most_rows > 8;
   if (p.idx != nullptr) {
-    if (D == 64) return wide ? launch_rows<64, 2, true>(p, scratch, grid, stream) : launch_rows<64, 1, true>(p, scratch, grid, stream);
-    return wide ? launch_rows<128, 2, true>(p, scratch, grid, stream) : launch_rows<128, 1, true>(p, scratch, grid, stream);
+    if (D == 64) return wide ? launch_rows<64, 2, true>(p, scratch, ctl, grid, stream) : launch_rows<64, 1, true>(p, scratch, ctl, grid, stream);
+    return wide ? launch_rows<128, 2, true>(p, scratch, ctl, grid, stream) : launch_rows<128, 1, true>(p, scratch, ctl, grid, stream);
   }
-  if (D == 64) return wide ? launch_rows<64, 2, false>(p, scratch, grid, stream) : launch_rows<64, 1, false>(p, scratch, grid, stream);
-  return wide ? launch_rows<128, 2, false>(p, scratch, grid, stream) : launch_rows<128, 1, false>(p, scratch, grid, stream);
+  if (D == 64) return wide ? launch_rows<64, 2, false>(p, scratch, ctl, grid, stream) : launch_rows<64, 1, false>(p, scratch, ctl, grid, stream);
+  return wide ? launch_rows<128, 2, false>(p, scratch, ctl, grid, stream) : launch_rows<128, 1, false>(p, scratch, ctl, grid, stream);
 }
 
 }  // namespace lt

@@ -36,6 +36,7 @@ __global__ void __launch_bounds__(kGenWarps * 32) attention_generic_kernel(const
   __shared__ float s_o[kGenWarps][D];
   __shared__ float s_m[kGenWarps], s_l[kGenWarps];
   const int t = blockIdx.x, h = blockIdx.y, kvh = h / p.group;
+  if (t == 0 && h == 0 && threadIdx.x < sizeof(Control) / 4) reinterpret_cast<int*>(p.ctl)[threadIdx.x] = 0;
   const int b = request_of(p, t);
   if (b < 0) return;
   const Kv4Request r = kv4_request(p, b);

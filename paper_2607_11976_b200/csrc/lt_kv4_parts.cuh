@@ -1,0 +1,221 @@
+// What the tensor-core attention kernels over the 4-bit cache share: arithmetic on codes, the running softmax, results and parts.
+#pragma once
+
+#include <type_traits>
+
+#include "lt_kv4.cuh"
+
+namespace lt {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// Probabilities are held times 2^11, relative to a maximum that is only raised when a score has passed it by 4 powers of two (raising
+// it multiplies all sums, and for 8 heads some score passes the exact maximum in every third unit): at most 2^15, and no less
+// than 2^-35 of the largest in fp16.
+constexpr float kPShift = 11.f, kPSlack = 4.f;
+constexpr float kNothing = 1e30f;  // shift of a row that has seen nothing
+
+// ---- arithmetic -------------------------------------------------------------------------------
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// A constant that stays in a register: instructions take one immediate, and the ones below would need two.
+__device__ __forceinline__ uint32_t held(uint32_t x) {
+  uint32_t r;
+  asm("mov.b32 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+struct ValueConstants {
+  uint32_t k1024, k16, inv16, minus72;
+  __device__ __forceinline__ ValueConstants() : k1024(held(0x64006400u)), k16(held(0x4C004C00u)), inv16(held(0x2C002C00u)), minus72(held(0xD480D480u)) {}
+};
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t c) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "r"(mask), "r"(c));
+  return d;
+}
+// Nibble i of each half of w as the fp16 pair (u - 8) s, rounded once; minus24s = -24 s.
+template <int i>
+__device__ __forceinline__ uint32_t f16_values(uint32_t w, uint32_t s, uint32_t minus24s, const ValueConstants& k) {
+  if constexpr (i == 0)
+    return hmul2(hadd2(and_or(w, 0x000F000Fu, k.k1024), 0xE408E408u), s);  // 1024 + u - 1032
+  else if constexpr (i == 1)
+    return hmul2(hfma2(and_or(w, 0x00F000F0u, k.k1024), k.inv16, k.minus72), s);  // (1024 + 16 u) / 16 - 72
+  else
+    return hfma2(and_or(w >> (4 * i - 6), 0x03C003C0u, k.k16), s, minus24s);  // 16 + u
+}
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t bf162_bits(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Quotient of counts that nearly always fit into 32 bits.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+  return a / b;
+}
+
+// Exclusive sum over the CTA's threads, and the total.
+template <int kWarps>
+__device__ __forceinline__ long long block_scan(long long v, long long& total, long long* warp_sums) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long inc = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, inc, d);
+    if (lane >= d) inc += x;
+  }
+  if (lane == 31) warp_sums[warp] = inc;
+  __syncthreads();
+  long long before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const long long x = warp_sums[w];
+    before += w < warp ? x : 0;
+    total += x;
+  }
+  __syncthreads();
+  return before + inc - v;
+}
+
+// ---- results ----------------------------------------------------------------------------------
+// Row r of an item's request (dense) or token (selected): where its query and result are.
+__device__ __forceinline__ void row_place(const Kv4AttnParams& p, int first, int kvh, int r, int& token, int& head) {
+  const int j = r / p.group;
+  token = first + j;
+  head = kvh * p.group + (r - j * p.group);
+}
+
+// 4 joined elements of a row and its sum: out, and lse once per row.
+template <int D>
+__device__ __forceinline__ void write_row4(const Kv4AttnParams& p, int token, int head, int d, const float4& o, float m, float l) {
+  const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
+  __nv_bfloat16* at = static_cast<__nv_bfloat16*>(p.out) + (static_cast<long long>(token) * p.Hq + head) * D + d;
+  *reinterpret_cast<uint2*>(at) = make_uint2(bf162_bits(o.x * inv, o.y * inv), bf162_bits(o.z * inv, o.w * inv));
+  if (d == 0 && p.lse != nullptr)
+    p.lse[static_cast<long long>(token) * p.Hq + head] = l > 0.f ? (m - kPShift + log2f(l)) * kLn2 : -INFINITY;
+}
+
+// (o, m, l) and another part of the same row: sums relative to the larger maximum.
+__device__ __forceinline__ void join(float4& o, float& m, float& l, const float4& x, float pm, float pl) {
+  const float mm = fmaxf(m, pm), a = m == -INFINITY ? 0.f : ex2(m - mm), b = pm == -INFINITY ? 0.f : ex2(pm - mm);
+  o = make_float4(o.x * a + x.x * b, o.y * a + x.y * b, o.z * a + x.z * b, o.w * a + x.w * b);
+  l = l * a + pl * b;
+  m = mm;
+}
+
+// ---- the parts of an item that several CTAs share --------------------------------------------------
+// A piece of an item: which rows, and whether it holds the item's first and last unit.
+struct PartDesc {
+  int b, kvh, rt, flags;
+};
+constexpr int kValid = 1, kBegins = 2, kEnds = 4;
+struct CtaDesc {
+  PartDesc part[2];  // [0] an item that began before this CTA's run, [1] one that begins in it and does not end
+  int status;        // LT_STATUS_* bits
+  int pad[7];
+};
+// Scratch of a call, one kernel pair after the other.
+struct SplitBuffers {
+  CtaDesc* desc;  // [grid]
+  float* cta;     // [grid][2] parts of kRows rows
+  float* warp;    // [grid][warps] parts: the first, incomplete item of a warp that goes on to others (few-row kernel)
+  Control* ctl;   // the call's status block
+};
+// Floats of a part: o[kRows][D], m[kRows] (powers of two), l[kRows].
+__host__ __device__ constexpr int part_floats(int rows, int D) { return rows * (D + 2); }
+
+// Items that span CTAs: CTA c joins the one that begins in run c with the pieces of the runs behind it.
+template <int D, int kRows, bool kTopk>
+__global__ void __launch_bounds__(256) attention_join_kernel(const Kv4AttnParams p, const SplitBuffers sb, int n_ctas, bool keep_status) {
+  constexpr int kFloats = part_floats(kRows, D);
+  chain_wait();
+  if (blockIdx.x == 0 && blockIdx.y == 0) {  // the call's status: what its CTAs left
+    __shared__ int s_status;
+    if (threadIdx.x == 0) s_status = keep_status ? sb.ctl->status : 0;
+    __syncthreads();
+    for (int c = threadIdx.x; c < n_ctas; c += 256)
+      if (sb.desc[c].status != 0) atomicOr(&s_status, sb.desc[c].status);
+    __syncthreads();
+    if (threadIdx.x < sizeof(Control) / 4) reinterpret_cast<int*>(sb.ctl)[threadIdx.x] = threadIdx.x == 0 ? s_status : 0;
+  }
+  const PartDesc run = sb.desc[blockIdx.x].part[1];
+  if (!(run.flags & kValid)) return;
+  // the CTAs behind this one that hold pieces of it: up to the first whose piece ends it
+  int n_more = 0;
+  for (int base = blockIdx.x + 1; base < n_ctas; base += 256) {
+    const int c = base + threadIdx.x;
+    const int flags = c < n_ctas ? sb.desc[c].part[0].flags : 0;
+    const bool ends = (flags & kEnds) != 0;
+    // (a run without units has no piece, and takes no part in the order)
+    __shared__ int s_end;
+    if (threadIdx.x == 0) s_end = n_ctas;
+    __syncthreads();
+    if (ends) atomicMin(&s_end, c);
+    __syncthreads();
+    n_more = (s_end < n_ctas ? s_end + 1 : n_ctas) - (blockIdx.x + 1);
+    const bool found = s_end < n_ctas;
+    __syncthreads();
+    if (found) break;
+  }
+  int first = run.b, rows = p.group;
+  if constexpr (!kTopk) {
+    const Kv4Request r = kv4_request(p, run.b);
+    first = r.first;
+    rows = r.n * p.group;
+  }
+  for (int v = blockIdx.y * 256 + threadIdx.x; v < kRows * D / 4; v += gridDim.y * 256) {
+    const int n = v * 4 / D, d = v * 4 % D, r = run.rt * kRows + n;
+    if (r >= rows) continue;
+    const float* part = sb.cta + (static_cast<long long>(blockIdx.x) * 2 + 1) * kFloats;
+    float4 o = *reinterpret_cast<const float4*>(part + n * D + d);
+    float m = part[kRows * D + n], l = part[kRows * D + kRows + n];
+    constexpr int kAhead = 8;  // pieces under way at once
+    for (int c0 = 0; c0 < n_more; c0 += kAhead) {
+      float4 x[kAhead];
+      float pm[kAhead], pl[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        pm[i] = -INFINITY;
+        pl[i] = 0.f;
+        const int c = blockIdx.x + 1 + c0 + i;
+        if (c0 + i < n_more && (sb.desc[c].part[0].flags & kValid)) {
+          part = sb.cta + static_cast<long long>(c) * 2 * kFloats;
+          x[i] = *reinterpret_cast<const float4*>(part + n * D + d);
+          pm[i] = part[kRows * D + n];
+          pl[i] = part[kRows * D + kRows + n];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) join(o, m, l, x[i], pm[i], pl[i]);
+    }
+    int token, head;
+    row_place(p, first, run.kvh, r, token, head);
+    write_row4<D>(p, token, head, d, o, m, l);
+  }
+}
+
+}  // namespace
+}  // namespace lt
