@@ -22,30 +22,35 @@
 namespace lt {
 namespace {
 
-constexpr int kTileRows = 128, kKeys = 128;
+constexpr int kTileRows = 128;
 constexpr int kStep = 32;       // rows of a stage of the ring
+constexpr int kKnown = 128;
 constexpr int kSeenStages = 4;  // tiles whose visible keys are noted at once
 
 template <int D, int kTiles>
 struct Cfg {
   static constexpr int kRow = kv4_row_bytes(D);
   static constexpr int kRows = kTiles * kTileRows;
-  static constexpr int kStages = kTiles == 2 ? 2 : 1;  // of unpacked keys, and of values
+  // Two tiles share 128 unpacked keys at a time, and one's product runs beside the other's softmax.  A single tile takes 64 keys and has
+  // S twice, so that its own next scores are there when a softmax ends.
+  static constexpr int kKeys = 64 * kTiles, kBufs = kTiles == 2 ? 1 : 2, kChunks = kKeys / 32;
+  static constexpr int kStages = 2;  // of unpacked keys, and of values
   static constexpr int kSoftmaxWarps = 4 * kTiles, kKeyWarp = kSoftmaxWarps, kValueWarp = kKeyWarp + 2, kMmaWarp = kValueWarp + 2,
                        kRowWarp = kMmaWarp + 1, kWarps = kRowWarp + 1, kThreads = kWarps * 32;
   static constexpr int kQueryBytes = kTileRows * D * 2, kTileBytes = kKeys * D * 2;  // queries; keys or values of one tile
   static constexpr int kRing = kTiles == 2 ? 6 : 3, kStepBytes = kStep * kRow;
   static constexpr size_t kSmem = 1024 + static_cast<size_t>(kQueryBytes) * kTiles + kTileBytes * 2 * kStages + kRing * kStepBytes;
   static constexpr int kCtasPerSm = kTiles == 2 ? 1 : 2;
-  static constexpr int kTmemCols = 256 * kTiles;  // S / P: 128 columns a tile, O: D (128 are taken)
+  static constexpr int kTmemCols = 256 * kTiles;  // S / P: 128 columns a tile (kBufs times kKeys), O: D (128 are taken)
 };
 
 struct Shared {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2][2], o_done[2], q_full[2], ring_full[6], ring_empty[6],
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_done[2], q_full[2], ring_full[6], ring_empty[6],
       seen_full[kSeenStages], seen_empty[kSeenStages], drained;
-  unsigned there[kSeenStages][kKeys / 32];  // a bit per key of the tile
+  unsigned there[kSeenStages][4];  // a bit per key of the tile
   int abort_flag[2], drain_flag[2];  // [1]: limit of a wait in microseconds (lt_ptx.cuh)
   uint32_t tmem;
+  long long units[kKnown];  // of one head of the first requests
   long long sums[16];
   // where the CTA's run begins
   long long lo, hi;
@@ -53,7 +58,7 @@ struct Shared {
 };
 
 // Items of a request (dense form): row tiles of kRows rows, each with the units of 128 keys that its last row sees.
-template <int kRows>
+template <int kRows, int kKeys>
 __device__ __forceinline__ int item_units(const Kv4AttnParams& p, const Kv4Request& r, int rt) {
   const long long rows = static_cast<long long>(r.n) * p.group, end = static_cast<long long>(rt + 1) * kRows;
   const int last = static_cast<int>(((end < rows ? end : rows) - 1) / p.group);
@@ -66,10 +71,10 @@ __device__ __forceinline__ int request_tiles(const Kv4AttnParams& p, const Kv4Re
   return rows < p.min_rows || rows > p.max_rows ? 0 : static_cast<int>((rows + kRows - 1) / kRows);
 }
 // Units of one key-value head of a request, summed by a warp.
-template <int kRows>
+template <int kRows, int kKeys>
 __device__ __forceinline__ long long request_units(const Kv4AttnParams& p, const Kv4Request& r, int tiles) {
   long long sum = 0;
-  for (int rt = threadIdx.x & 31; rt < tiles; rt += 32) sum += item_units<kRows>(p, r, rt);
+  for (int rt = threadIdx.x & 31; rt < tiles; rt += 32) sum += item_units<kRows, kKeys>(p, r, rt);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   return sum;
@@ -78,7 +83,7 @@ __device__ __forceinline__ long long request_units(const Kv4AttnParams& p, const
 // Where a role stands: every role walks through the CTA's run by itself.
 template <int D, int kTiles, bool kTopk>
 struct Walk {
-  static constexpr int kRows = Cfg<D, kTiles>::kRows;
+  static constexpr int kRows = Cfg<D, kTiles>::kRows, kKeys = Cfg<D, kTiles>::kKeys;
   int b, kvh, rt, unit, units, tiles;
   long long left;
   Kv4Request r;
@@ -98,7 +103,7 @@ struct Walk {
     } else {
       r = kv4_request(p, b);
       tiles = request_tiles<kRows>(p, r);
-      units = tiles > 0 ? item_units<kRows>(p, r, rt) : 0;
+      units = tiles > 0 ? item_units<kRows, kKeys>(p, r, rt) : 0;
     }
   }
   // the item's units that are in the run: unit .. end() - 1
@@ -108,12 +113,12 @@ struct Walk {
     if (left <= 0) return false;
     unit = 0;
     if (++rt < tiles) {
-      if constexpr (!kTopk) units = item_units<kRows>(p, r, rt);
+      if constexpr (!kTopk) units = item_units<kRows, kKeys>(p, r, rt);
       return true;
     }
     rt = 0;
     if (++kvh < p.Hkv) {
-      if constexpr (!kTopk) units = item_units<kRows>(p, r, 0);
+      if constexpr (!kTopk) units = item_units<kRows, kKeys>(p, r, 0);
       return true;
     }
     kvh = 0;
@@ -142,12 +147,26 @@ struct Turn {
   }
 };
 
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
-      "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+        "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
       : "memory");
+}
+// The wait names the registers, so that no use of them moves above it.
+__device__ __forceinline__ void tmem_ld16_wait(uint32_t (&v)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                 "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
   asm volatile(
@@ -158,7 +177,50 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32
       "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
       : "memory");
 }
+__device__ __forceinline__ unsigned long long pack2(float a, float b) {
+  unsigned long long x;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
+  return x;
+}
+__device__ __forceinline__ void unpack2(unsigned long long x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Bounded wait, as ptx::mbar_wait, of a role with nothing else to do: the warp is suspended for up to 20 us at a time.  (Ten warps of
+// an SM polling at will took 40 % of its issue slots.)
+__device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  uint64_t t0 = 0;
+  while (true) {
+    uint32_t done;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(done)
+        : "r"(bar), "r"(parity), "r"(20000u)
+        : "memory");
+    if (done) return true;
+    if (*abort_flag) return false;
+    const uint64_t now = ptx::globaltimer_ns();
+    if (t0 == 0) {
+      t0 = now;
+    } else if (now - t0 > static_cast<uint64_t>(static_cast<uint32_t>(abort_flag[1])) * 1000ull) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+}
+
 // Products and their signals are issued by one lane, the same every time, from code that all lanes run: operands then live in uniform
 // registers.  (With one lane in a branch of its own each product cost some 110 clocks to issue.)
 // D[tmem] (+)= A[smem] * B[smem]^T
@@ -245,6 +307,20 @@ __device__ __forceinline__ uint4 lds_codes(uint32_t at) {
   return x;
 }
 
+// A warp's rows of O times a factor each.  (Out of line it cost 5 %.)
+template <int D>
+__device__ __forceinline__ void scale_rows(uint32_t t_o, float back) {
+#pragma unroll 1
+  for (int chunk = 0; chunk < D / 32; ++chunk) {
+    uint32_t v[32];
+    ptx::tmem_ld32(t_o + chunk * 32, v);
+    ptx::tmem_ld_wait(v);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * back);
+    tmem_st32(t_o + chunk * 32, v);
+  }
+}
+
 // ---------------------------------------------------------------------------------------------
 template <int D, int kTiles, bool kTopk>
 __global__ void __launch_bounds__(Cfg<D, kTiles>::kThreads, Cfg<D, kTiles>::kCtasPerSm)
@@ -257,6 +333,7 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t s_q = base, s_k = s_q + kTiles * C::kQueryBytes, s_v = s_k + C::kStages * C::kTileBytes, s_ring = s_v + C::kStages * C::kTileBytes;
   auto bar = [&](uint64_t& b) { return ptx::smem_u32(&b); };
+  constexpr int kKeys = C::kKeys;
   constexpr uint32_t kHalfQ = kTileRows * 128, kHalfK = kKeys * 128, kHalfV = D * 128;  // bytes of 64 elements of the rows
   constexpr int kUnpackers = 64;
 
@@ -268,8 +345,10 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
       ptx::mbar_init(bar(sh.v_empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(bar(sh.s_full[i]), 1);
-      for (int j = 0; j < 2; ++j) ptx::mbar_init(bar(sh.p_full[i][j]), kTileRows);
+      for (int j = 0; j < 2; ++j) {
+        ptx::mbar_init(bar(sh.s_full[i][j]), 1);
+        ptx::mbar_init(bar(sh.p_full[i][j]), kTileRows);
+      }
       ptx::mbar_init(bar(sh.o_done[i]), 1);
       ptx::mbar_init(bar(sh.q_full[i]), kTileRows);
     }
@@ -328,42 +407,58 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
         }
       }
     } else {
-      // the total: a request per warp and turn
+      // the total: a request per warp and turn; what a head of the first ones takes is kept
       long long sum = 0;
       for (int b = warp; b < p.B; b += C::kWarps) {
         const Kv4Request r = kv4_request(p, b);
         const int tiles = request_tiles<C::kRows>(p, r);
-        if (tiles > 0) sum += request_units<C::kRows>(p, r, tiles) * p.Hkv;
+        const long long per = tiles > 0 ? request_units<C::kRows, kKeys>(p, r, tiles) : 0;
+        if (lane == 0 && b < kKnown) sh.units[b] = per;
+        sum += per * p.Hkv;
       }
       if (lane == 0) sh.sums[warp] = sum;
       __syncthreads();
       if (warp == 0) {
-        long long total = 0, lo, hi;
+        long long total = 0, lo, hi, before = 0, per = 0;
         for (int w = 0; w < C::kWarps; ++w) total += sh.sums[w];
         cut(total, lo, hi);
-        long long before = 0;
-        for (int b = 0; lo < hi && b < p.B; ++b) {
+        int b = 0;
+        for (; lo < hi && b < p.B; ++b) {
+          if (b < kKnown) {
+            per = sh.units[b];
+          } else {
+            const Kv4Request r = kv4_request(p, b);
+            const int tiles = request_tiles<C::kRows>(p, r);
+            per = tiles > 0 ? request_units<C::kRows, kKeys>(p, r, tiles) : 0;
+          }
+          if (lo < before + per * p.Hkv) break;
+          before += per * p.Hkv;
+        }
+        if (lo < hi) {
           const Kv4Request r = kv4_request(p, b);
-          const int tiles = request_tiles<C::kRows>(p, r);
-          if (tiles == 0) continue;
-          const long long per = request_units<C::kRows>(p, r, tiles);
-          if (lo >= before + per * p.Hkv) {
-            before += per * p.Hkv;
-            continue;
-          }
           const int kvh = static_cast<int>(quotient(lo - before, per));
-          long long off = lo - before - per * kvh;
-          int rt = 0;
-          for (int units; off >= (units = item_units<C::kRows>(p, r, rt)); ++rt) off -= units;
-          if (lane == 0) {
-            sh.lo = lo;
-            sh.hi = hi;
-            sh.b = b;
-            sh.kvh = kvh;
-            sh.rt = rt;
-            sh.unit = static_cast<int>(off);
+          const long long off = lo - before - per * kvh;
+          long long passed = 0;  // units of the tiles before, 32 tiles at a look
+          for (int rt0 = 0;; rt0 += 32) {
+            const int tiles = request_tiles<C::kRows>(p, r), rt = rt0 + lane, mine = rt < tiles ? item_units<C::kRows, kKeys>(p, r, rt) : 0;
+            int inc = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+              const int x = __shfl_up_sync(0xffffffffu, inc, d);
+              if (lane >= d) inc += x;
+            }
+            const bool here = off < passed + inc && off >= passed + inc - mine;
+            if (here) {
+              sh.lo = lo;
+              sh.hi = hi;
+              sh.b = b;
+              sh.kvh = kvh;
+              sh.rt = rt;
+              sh.unit = static_cast<int>(off - (passed + inc - mine));
+            }
+            if (__any_sync(0xffffffffu, here) || rt0 + 32 >= tiles) break;
+            passed += __shfl_sync(0xffffffffu, inc, 31);
           }
-          break;
         }
       }
     }
@@ -378,9 +473,346 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
   }
   __syncthreads();
 
-  if (!any) {
-    // nothing to do
-  } else if (warp == C::kRowWarp) {
+  if (warp < C::kSoftmaxWarps) {
+    if (any) {
+    // ---- softmax ---------------------------------------------------------------------------------------
+    const int tt = warp >> 2, r128 = (warp & 3) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + lanes + tt * 128, t_o = tmem + lanes + kTiles * 128 + tt * 128;
+    const float to_log2 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);
+    Turn<kSeenStages> seen;
+    uint32_t s_phase[2] = {0, 0}, o_phase = 0;
+    int buf = 0;
+    bool more = true, ok = true;
+    while (more) {
+      // the row's query, its largest element in [2^15, 2^16), elements paired as the codes are
+      const int rows = kTopk ? p.group : at.r.n * p.group, r0 = at.rt * C::kRows + tt * kTileRows, r = r0 + r128;
+      int token = 0, head = 0;
+      float worth = 1.f;
+      // (a tile without rows takes no part; a warp without any keeps step and computes nothing)
+      const bool tile_there = r0 < rows, warp_there = r0 + (warp & 3) * 32 < rows;
+      if (tile_there) {
+        const uint32_t to = s_q + tt * C::kQueryBytes;
+        const uint4* src = nullptr;
+        if (r < rows) {
+          row_place(p, at.r.first, at.kvh, r, token, head);
+          src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + token * p.q_stride + static_cast<long long>(head) * D);
+        }
+        uint32_t top = 0;
+        if (src != nullptr) {
+#pragma unroll 4
+          for (int i = 0; i < D / 8; ++i) {
+            const uint4 x = __ldg(src + i);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
+          }
+        }
+        const int e = max(static_cast<int>(top >> 7), 21);
+        const float up = copysignf(__uint_as_float(static_cast<uint32_t>(127 + 127 + 15 - e) << 23), p.scale);
+        worth = fminf(__uint_as_float(static_cast<uint32_t>(e - 15) << 23) * to_log2, 0x1p80f);
+#pragma unroll 4
+        for (int i = 0; i < D / 8; ++i) {
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (src != nullptr) x = __ldg(src + i);
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          float f[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            f[2 * j] = __uint_as_float(w[j] << 16) * up;
+            f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u) * up;
+          }
+          sts128(to + (i >> 3) * kHalfQ + swizzled(r128, i & 7), half2_bits(f[0], f[4]), half2_bits(f[1], f[5]), half2_bits(f[2], f[6]),
+                 half2_bits(f[3], f[7]));
+        }
+        ptx::fence_proxy_async();
+        ptx::tc_fence_before();  // (the item before has been read from tensor memory)
+        ptx::mbar_arrive(bar(sh.q_full[tt]));
+      }
+      // how far the row, and the tile's first row, see (dense form)
+      const long long limit = static_cast<long long>(at.r.ctx) + (r < rows ? r : rows - 1) / p.group;
+      const long long least = static_cast<long long>(at.r.ctx) + (r0 < rows ? r0 : rows - 1) / p.group;
+      float worth_bar = -INFINITY, shift = kNothing, l = 0.f;
+      const int unit0 = at.unit, unit1 = at.end();
+      for (int unit = unit0; unit < unit1 && ok; ++unit) {
+        ok = long_wait(bar(sh.seen_full[seen.i]), seen.phase, gave_up);
+        if (!__all_sync(0xffffffffu, ok)) {  // (a warp goes on, or gives up, as one)
+          ok = false;
+          break;
+        }
+        unsigned there[C::kChunks], all = 0xffffffffu;
+#pragma unroll
+        for (int i = 0; i < C::kChunks; ++i) {
+          there[i] = sh.there[seen.i][i];
+          all &= there[i];
+        }
+        ptx::mbar_arrive(bar(sh.seen_empty[seen.i]));
+        seen.next();
+        if (!tile_there) continue;
+        const bool whole = all == 0xffffffffu && (kTopk || static_cast<long long>(unit) * kKeys + kKeys - 1 <= least);
+        ok = long_wait(bar(sh.s_full[tt][buf]), s_phase[buf], gave_up);
+        s_phase[buf] ^= 1;
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          break;
+        }
+        const uint32_t t_sb = t_s + buf * kKeys;
+        if (!warp_there) {
+          ptx::mbar_arrive(bar(sh.p_full[tt][buf]));
+          if (C::kBufs == 1) ptx::mbar_arrive(bar(sh.p_full[tt][1]));
+          if (C::kBufs == 2) buf ^= 1;
+          o_phase ^= 1;
+          continue;
+        }
+        ptx::tc_fence_after();
+        // S is read twice, 32 columns at a time: short loops, and few registers
+        auto hide = [&](uint32_t (&v)[16], int c16) {  // column 8 m + i is key 8 m + (m + i) % 8
+          const long long left = limit - (static_cast<long long>(unit) * kKeys + c16 * 16);
+          unsigned sees = there[0];
+#pragma unroll
+          for (int i = 1; i < C::kChunks; ++i) sees = c16 / 2 == i ? there[i] : sees;
+          sees >>= (c16 & 1) * 16;
+          if constexpr (!kTopk) sees = left >= 15 ? sees : left < 0 ? 0u : sees & (0xffffu >> (15 - static_cast<int>(left)));
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = (i & 8) + ((c16 * 2 + (i >> 3) + i) & 7);
+            if (!((sees >> key) & 1u)) v[i] = 0xff800000u;
+          }
+        };
+        constexpr int kN = C::kKeys / 16;
+        uint32_t x[16], y[16];
+        float tops[2] = {-INFINITY, -INFINITY};
+        auto raise = [&](const uint32_t (&v)[16]) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            tops[0] = fmaxf(fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), tops[0]);
+            tops[1] = fmaxf(fmaxf(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), tops[1]);
+          }
+        };
+        // (loops of their own for units that are seen whole: a test in the loop became selects that ran every time)
+        auto first_reading = [&](auto whole_unit) {
+          constexpr bool kWhole = decltype(whole_unit)::value;
+#pragma unroll 1
+          for (int c = 0; c < kN; c += 2) {
+            tmem_ld16(t_sb + c * 16, x);
+            tmem_ld16(t_sb + c * 16 + 16, y);
+            tmem_ld16_wait(x);
+            tmem_ld16_wait(y);
+            if constexpr (!kWhole) hide(x, c);
+            if constexpr (!kWhole) hide(y, c + 1);
+            raise(x);
+            raise(y);
+          }
+        };
+        if (__builtin_expect(whole, 1))
+          first_reading(std::true_type{});
+        else
+          first_reading(std::false_type{});
+        const float top = fmaxf(tops[0], tops[1]);
+        const bool grows = top > worth_bar;
+        if (__builtin_expect(__any_sync(0xffffffffu, grows), 0)) {
+          float back = 1.f;
+          if (grows) {
+            const float now = kPShift - top * worth;
+            back = ex2(now - shift);
+            worth_bar = top + kPSlack / worth;
+            shift = now;
+            l *= back;
+          }
+          if (unit > unit0) {  // what there is of O, once the product before is through
+            ok = long_wait(bar(sh.o_done[tt]), o_phase ^ 1, gave_up);
+            if (!__all_sync(0xffffffffu, ok)) {
+              ok = false;
+              break;
+            }
+            ptx::tc_fence_after();
+            scale_rows<D>(t_o, back);
+          }
+        }
+        // p = 2^(worth s + shift), two at a time where the pipes allow
+        const unsigned long long worth2 = pack2(worth, worth), shift2 = pack2(shift, shift);
+        unsigned long long sum = 0;
+        auto exponentials = [&](const uint32_t (&v)[16], int c) {
+          uint32_t h[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const unsigned long long e = fma2(pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), worth2, shift2);
+            float a, b;
+            unpack2(e, a, b);
+            a = ex2(a);
+            b = ex2(b);
+            sum = add2(sum, pack2(a, b));
+            h[i] = half2_bits(a, b);
+          }
+          tmem_st8(t_sb + c * 8, h);
+        };
+        auto second_reading = [&](auto whole_unit) {
+          constexpr bool kWhole = decltype(whole_unit)::value;
+#pragma unroll 1
+          for (int c = 0; c < kN; c += 2) {
+            tmem_ld16(t_sb + c * 16, x);
+            tmem_ld16(t_sb + c * 16 + 16, y);
+            tmem_ld16_wait(x);
+            tmem_ld16_wait(y);
+            if constexpr (!kWhole) hide(x, c);
+            if constexpr (!kWhole) hide(y, c + 1);
+            exponentials(x, c);
+            exponentials(y, c + 1);
+            if ((c & 3) == 2) {  // 64 keys: their product may begin
+              tmem_st_wait();
+              ptx::tc_fence_before();
+              ptx::mbar_arrive(bar(sh.p_full[tt][C::kBufs == 2 ? buf : c >> 2]));
+            }
+          }
+        };
+        if (__builtin_expect(whole, 1))
+          second_reading(std::true_type{});
+        else
+          second_reading(std::false_type{});
+        float sum0, sum1;
+        unpack2(sum, sum0, sum1);
+        l += sum0 + sum1;
+        if (C::kBufs == 2) buf ^= 1;
+        o_phase ^= 1;
+      }
+      if (!ok) break;
+      // the item's end, or the run's
+      if (tile_there) ok = long_wait(bar(sh.o_done[tt]), o_phase ^ 1, gave_up);
+      if (!__all_sync(0xffffffffu, ok)) {
+        ok = false;
+        break;
+      }
+      ptx::tc_fence_after();
+      const bool begins = unit0 == 0, ends = unit1 == at.units;
+      const float m = l > 0.f ? kPShift - shift : -INFINITY;
+      float* part = sb.cta + (static_cast<long long>(blockIdx.x) * 2 + (begins ? 1 : 0)) * part_floats(C::kRows, D);
+      const int n = tt * kTileRows + r128;
+#pragma unroll 1
+      for (int chunk = 0; warp_there && chunk < D / 32; ++chunk) {
+        uint32_t v[32];
+        ptx::tmem_ld32(t_o + chunk * 32, v);
+        ptx::tmem_ld_wait(v);
+        if (begins && ends) {
+          if (r < rows) {
+            const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
+            uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + (static_cast<long long>(token) * p.Hq + head) * D + chunk * 32);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t h[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                h[j] = bf162_bits(__uint_as_float(v[i * 8 + j * 2]) * inv, __uint_as_float(v[i * 8 + j * 2 + 1]) * inv);
+              to[i] = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4*>(part + n * D + chunk * 32 + i * 4) = make_uint4(v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3]);
+        }
+      }
+      if (begins && ends) {
+        if (r < rows && p.lse != nullptr)
+          p.lse[static_cast<long long>(token) * p.Hq + head] = l > 0.f ? (m - kPShift + log2f(l)) * kLn2 : -INFINITY;
+      } else {
+        if (warp_there) {
+          part[C::kRows * D + n] = m;
+          part[C::kRows * D + C::kRows + n] = l;
+        }
+        if (tid == 0)
+          sb.desc[blockIdx.x].part[begins ? 1 : 0] = PartDesc{at.b, at.kvh, at.rt, kValid | (begins ? kBegins : 0) | (ends ? kEnds : 0)};
+      }
+      more = at.next(p);
+    }
+    }
+  } else if (warp < C::kMmaWarp) {
+    if (any && warp < C::kValueWarp) {
+    // ---- keys: lane = group * 8 + x handles that group of 8 neighbouring keys; D = 64 has two groups, and half of the lanes take the
+    // next eight ------------------------------------------------------------------------------------------
+    constexpr int kGroups = D / kKvGroup, kOctets = 4 / kGroups;  // octets of keys a warp takes at once
+    const int x = lane & 7, gi = (lane >> 3) % kGroups, o0 = (warp - C::kKeyWarp) * kOctets + (lane >> 3) / kGroups;
+    const ValueConstants constants;
+    Turn<C::kRing> ring;
+    Turn<C::kStages> k;
+    bool ok = true;
+    for (long long left = sh.hi - sh.lo; left > 0 && ok; --left) {
+      ok = long_wait(bar(sh.k_empty[k.i]), k.phase ^ 1, gave_up);
+      const uint32_t to = s_k + k.i * C::kTileBytes + (gi >> 1) * kHalfK;
+#pragma unroll 1
+      for (int step = 0; step < kKeys / kStep && ok; ++step) {
+        ok = long_wait(bar(sh.ring_full[ring.i]), ring.phase, gave_up);
+#pragma unroll 1
+        for (int o = o0; o < kStep / 8; o += 2 * kOctets) {
+          const uint32_t from = s_ring + ring.i * C::kStepBytes + (o * 8 + x) * C::kRow;
+          const int m = step * (kStep / 8) + o, c = m * 8 + ((x - m) & 7);  // column of key 8 m + x
+          const uint4 codes = lds_codes<C::kRow>(from + gi * 16);
+          const uint32_t scale = lds16(from + D + gi * 2), s2 = scale | (scale << 16), c2 = hfma2(s2, 0xCE00CE00u, 0u);  // -24 s
+          const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            sts128(to + swizzled(c, (gi & 1) * 4 + j), f16_values<0>(w[j], s2, c2, constants), f16_values<1>(w[j], s2, c2, constants),
+                   f16_values<2>(w[j], s2, c2, constants), f16_values<3>(w[j], s2, c2, constants));
+        }
+        ptx::mbar_arrive(bar(sh.ring_empty[ring.i]));
+        ring.next();
+      }
+      ptx::fence_proxy_async();
+      ptx::mbar_arrive(bar(sh.k_full[k.i]));
+      k.next();
+    }
+    } else if (any) {
+    // ---- values: a lane handles a code word of the 8 keys of a piece (4 pieces a step); of D = 128 each warp takes half of the words, of
+    // D = 64 every other step -----------------------------------------------------------------------------
+    const int v_warp = warp - C::kValueWarp, word = (lane >> 2) + (D == 128 ? v_warp * 8 : 0);
+    const ValueConstants constants;
+    Turn<C::kRing> ring;
+    Turn<C::kStages> v;
+    bool ok = true;
+    for (long long left = sh.hi - sh.lo; left > 0 && ok; --left) {
+      ok = long_wait(bar(sh.v_empty[v.i]), v.phase ^ 1, gave_up);
+#pragma unroll 1
+      for (int step = 0; step < kKeys / kStep && ok; ++step) {
+        ok = long_wait(bar(sh.ring_full[ring.i]), ring.phase, gave_up);
+        if (D == 128 || (step & 1) == v_warp) {
+          const int m = step * (kStep / 8) + (lane & 3);
+          const uint32_t from = s_ring + ring.i * C::kStepBytes + (lane & 3) * 8 * C::kRow;
+          uint32_t lo16[4], hi16[4], s2[4], c2[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {  // columns 2 q and 2 q + 1 of the piece
+            const uint32_t r0 = from + ((m + 2 * q) & 7) * C::kRow, r1 = from + ((m + 2 * q + 1) & 7) * C::kRow;
+            const uint32_t a = lds32(r0 + D / 2 + word * 4), b = lds32(r1 + D / 2 + word * 4);
+            s2[q] = lds16(r0 + D + D / 16 + (word >> 2) * 2) | (lds16(r1 + D + D / 16 + (word >> 2) * 2) << 16);
+            c2[q] = hfma2(s2[q], 0xCE00CE00u, 0u);
+            lo16[q] = __byte_perm(a, b, 0x5410);
+            hi16[q] = __byte_perm(a, b, 0x7632);
+          }
+          const uint32_t to = s_v + v.i * C::kTileBytes + (m >> 3) * kHalfV + word * 8 * 128;
+          auto put = [&](auto e) {
+            constexpr int kE = decltype(e)::value;
+            const uint32_t(&src)[4] = kE < 4 ? lo16 : hi16;
+            sts128(to + swizzled(kE, m & 7), f16_values<kE % 4>(src[0], s2[0], c2[0], constants),
+                   f16_values<kE % 4>(src[1], s2[1], c2[1], constants), f16_values<kE % 4>(src[2], s2[2], c2[2], constants),
+                   f16_values<kE % 4>(src[3], s2[3], c2[3], constants));
+          };
+          put(std::integral_constant<int, 0>{});
+          put(std::integral_constant<int, 1>{});
+          put(std::integral_constant<int, 2>{});
+          put(std::integral_constant<int, 3>{});
+          put(std::integral_constant<int, 4>{});
+          put(std::integral_constant<int, 5>{});
+          put(std::integral_constant<int, 6>{});
+          put(std::integral_constant<int, 7>{});
+        }
+        ptx::mbar_arrive(bar(sh.ring_empty[ring.i]));
+        ring.next();
+      }
+      ptx::fence_proxy_async();
+      ptx::mbar_arrive(bar(sh.v_full[v.i]));
+      v.next();
+    }
+    }
+  } else {
+    if (any && warp == C::kRowWarp) {
     // ---- rows: a lane has a key of each step; the next tile's positions and pages are looked up while this one's are copied -----------
     Turn<C::kRing> ring;
     Turn<kSeenStages> seen;
@@ -457,7 +889,7 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
         }
         look_up(unit);
       }
-      ok = ptx::mbar_wait<64>(bar(sh.seen_empty[seen.i]), seen.phase ^ 1, gave_up);
+      ok = long_wait(bar(sh.seen_empty[seen.i]), seen.phase ^ 1, gave_up);
       if (lane == 0 && ok) {
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) sh.there[seen.i][i] = there[i];
@@ -466,7 +898,7 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
       seen.next();
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        ok = ok && ptx::mbar_wait<64>(bar(sh.ring_empty[ring.i]), ring.phase ^ 1, gave_up);
+        ok = ok && long_wait(bar(sh.ring_empty[ring.i]), ring.phase ^ 1, gave_up);
         if (!__all_sync(0xffffffffu, ok)) {
           ok = false;
           break;
@@ -498,356 +930,104 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
     // no copy is under way when the CTA ends, also where a role gave up
     for (int i = 0; i < C::kRing; ++i) {
       const int n = (issued - i + C::kRing - 1) / C::kRing;  // uses of stage i
-      if (issued > i) ptx::mbar_wait<64>(bar(sh.ring_full[i]), static_cast<uint32_t>((n - 1) & 1), sh.drain_flag);
+      if (issued > i) long_wait(bar(sh.ring_full[i]), static_cast<uint32_t>((n - 1) & 1), sh.drain_flag);
     }
-  } else if (warp >= C::kKeyWarp && warp < C::kValueWarp) {
-    // ---- keys: lane = group * 8 + x handles that group of 8 neighbouring keys; D = 64 has two groups, and half of the lanes take the
-    // next eight ------------------------------------------------------------------------------------------
-    constexpr int kGroups = D / kKvGroup, kOctets = 4 / kGroups;  // octets of keys a warp takes at once
-    const int x = lane & 7, gi = (lane >> 3) % kGroups, o0 = (warp - C::kKeyWarp) * kOctets + (lane >> 3) / kGroups;
-    const ValueConstants constants;
-    Turn<C::kRing> ring;
-    Turn<C::kStages> k;
-    bool ok = true;
-    for (long long left = sh.hi - sh.lo; left > 0 && ok; --left) {
-      ok = ptx::mbar_wait(bar(sh.k_empty[k.i]), k.phase ^ 1, gave_up);
-      const uint32_t to = s_k + k.i * C::kTileBytes + (gi >> 1) * kHalfK;
-#pragma unroll 1
-      for (int step = 0; step < kKeys / kStep && ok; ++step) {
-        ok = ptx::mbar_wait(bar(sh.ring_full[ring.i]), ring.phase, gave_up);
-#pragma unroll 1
-        for (int o = o0; o < kStep / 8; o += 2 * kOctets) {
-          const uint32_t from = s_ring + ring.i * C::kStepBytes + (o * 8 + x) * C::kRow;
-          const int m = step * (kStep / 8) + o, c = m * 8 + ((x - m) & 7);  // column of key 8 m + x
-          const uint4 codes = lds_codes<C::kRow>(from + gi * 16);
-          const uint32_t scale = lds16(from + D + gi * 2), s2 = scale | (scale << 16), c2 = hfma2(s2, 0xCE00CE00u, 0u);  // -24 s
-          const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            sts128(to + swizzled(c, (gi & 1) * 4 + j), f16_values<0>(w[j], s2, c2, constants), f16_values<1>(w[j], s2, c2, constants),
-                   f16_values<2>(w[j], s2, c2, constants), f16_values<3>(w[j], s2, c2, constants));
-        }
-        ptx::mbar_arrive(bar(sh.ring_empty[ring.i]));
-        ring.next();
-      }
-      ptx::fence_proxy_async();
-      ptx::mbar_arrive(bar(sh.k_full[k.i]));
-      k.next();
-    }
-  } else if (warp >= C::kValueWarp && warp < C::kMmaWarp) {
-    // ---- values: a lane handles a code word of the 8 keys of a piece (4 pieces a step); of D = 128 each warp takes half of the words, of
-    // D = 64 every other step -----------------------------------------------------------------------------
-    const int v_warp = warp - C::kValueWarp, word = (lane >> 2) + (D == 128 ? v_warp * 8 : 0);
-    const ValueConstants constants;
-    Turn<C::kRing> ring;
-    Turn<C::kStages> v;
-    bool ok = true;
-    for (long long left = sh.hi - sh.lo; left > 0 && ok; --left) {
-      ok = ptx::mbar_wait(bar(sh.v_empty[v.i]), v.phase ^ 1, gave_up);
-#pragma unroll 1
-      for (int step = 0; step < kKeys / kStep && ok; ++step) {
-        ok = ptx::mbar_wait(bar(sh.ring_full[ring.i]), ring.phase, gave_up);
-        if (D == 128 || (step & 1) == v_warp) {
-          const int m = step * (kStep / 8) + (lane & 3);
-          const uint32_t from = s_ring + ring.i * C::kStepBytes + (lane & 3) * 8 * C::kRow;
-          uint32_t lo16[4], hi16[4], s2[4], c2[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {  // columns 2 q and 2 q + 1 of the piece
-            const uint32_t r0 = from + ((m + 2 * q) & 7) * C::kRow, r1 = from + ((m + 2 * q + 1) & 7) * C::kRow;
-            const uint32_t a = lds32(r0 + D / 2 + word * 4), b = lds32(r1 + D / 2 + word * 4);
-            s2[q] = lds16(r0 + D + D / 16 + (word >> 2) * 2) | (lds16(r1 + D + D / 16 + (word >> 2) * 2) << 16);
-            c2[q] = hfma2(s2[q], 0xCE00CE00u, 0u);
-            lo16[q] = __byte_perm(a, b, 0x5410);
-            hi16[q] = __byte_perm(a, b, 0x7632);
-          }
-          const uint32_t to = s_v + v.i * C::kTileBytes + (m >> 3) * kHalfV + word * 8 * 128;
-          auto put = [&](auto e) {
-            constexpr int kE = decltype(e)::value;
-            const uint32_t(&src)[4] = kE < 4 ? lo16 : hi16;
-            sts128(to + swizzled(kE, m & 7), f16_values<kE % 4>(src[0], s2[0], c2[0], constants),
-                   f16_values<kE % 4>(src[1], s2[1], c2[1], constants), f16_values<kE % 4>(src[2], s2[2], c2[2], constants),
-                   f16_values<kE % 4>(src[3], s2[3], c2[3], constants));
-          };
-          put(std::integral_constant<int, 0>{});
-          put(std::integral_constant<int, 1>{});
-          put(std::integral_constant<int, 2>{});
-          put(std::integral_constant<int, 3>{});
-          put(std::integral_constant<int, 4>{});
-          put(std::integral_constant<int, 5>{});
-          put(std::integral_constant<int, 6>{});
-          put(std::integral_constant<int, 7>{});
-        }
-        ptx::mbar_arrive(bar(sh.ring_empty[ring.i]));
-        ring.next();
-      }
-      ptx::fence_proxy_async();
-      ptx::mbar_arrive(bar(sh.v_full[v.i]));
-      v.next();
-    }
-  } else if (warp == C::kMmaWarp) {
+    } else if (any && warp == C::kMmaWarp) {
     // ---- products --------------------------------------------------------------------------------------
     {
       Turn<C::kStages> k, v;
-      uint32_t q_phase = 0, p_phase = 0, o_phase = 0;
-      auto wait = [&](uint64_t& b, uint32_t phase) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar(b), phase, gave_up)) != 0; };
-      auto scores = [&](int tt) {
+      uint32_t q_phase[2] = {0, 0}, o_phase[2] = {0, 0}, p_phase[2][2] = {{0, 0}, {0, 0}};
+      auto wait = [&](uint64_t& b, uint32_t phase) { return __all_sync(0xffffffffu, long_wait(bar(b), phase, gave_up)) != 0; };
+      auto scores = [&](int tt, int buf) {
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)
-          mma_from_smem(tmem + tt * 128, ptx::make_smem_desc_sw128(s_q + tt * C::kQueryBytes + (s >> 2) * kHalfQ + (s & 3) * 32),
+          mma_from_smem(tmem + tt * 128 + buf * kKeys, ptx::make_smem_desc_sw128(s_q + tt * C::kQueryBytes + (s >> 2) * kHalfQ + (s & 3) * 32),
                         ptx::make_smem_desc_sw128(s_k + k.i * C::kTileBytes + (s >> 2) * kHalfK + (s & 3) * 32), f16_idesc(kKeys), s > 0);
-        commit(bar(sh.s_full[tt]));
+        commit(bar(sh.s_full[tt][buf]));
       };
-      auto values = [&](int tt, int half, bool more) {
+      auto values = [&](int tt, int col, int half, bool more) {  // 64 keys
 #pragma unroll
         for (int s = 0; s < 4; ++s)
-          mma_from_tmem(tmem + kTiles * 128 + tt * 128, tmem + tt * 128 + half * 32 + s * 8,
+          mma_from_tmem(tmem + kTiles * 128 + tt * 128, tmem + tt * 128 + col + s * 8,
                         ptx::make_smem_desc_sw128(s_v + v.i * C::kTileBytes + half * kHalfV + s * 32), f16_idesc(D), more || s > 0);
       };
       bool more = true, ok = true;
+      int buf = 0;
       while (more && ok) {
         const int n = at.end() - at.unit;
-#pragma unroll
-        for (int tt = 0; tt < kTiles; ++tt) ok = ok && wait(sh.q_full[tt], q_phase);
-        q_phase ^= 1;
-        ok = ok && wait(sh.k_full[k.i], k.phase);
-        if (!ok) break;
-        ptx::tc_fence_after();
-#pragma unroll
-        for (int tt = 0; tt < kTiles; ++tt) scores(tt);
-        commit(bar(sh.k_empty[k.i]));
-        k.next();
-        for (int j = 0; j < n && ok; ++j) {
-          const bool ahead = j + 1 < n;
-          ok = wait(sh.v_full[v.i], v.phase);
-#pragma unroll
-          for (int tt = 0; tt < kTiles; ++tt) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              ok = ok && wait(sh.p_full[tt][half], p_phase);
+        // (a second tile without rows is left out)
+        const int nt = kTiles == 2 && !kTopk && static_cast<long long>(at.r.n) * p.group <= at.rt * C::kRows + kTileRows ? 1 : kTiles;
+        for (int tt = 0; tt < nt; ++tt) {
+          ok = ok && wait(sh.q_full[tt], q_phase[tt]);
+          q_phase[tt] ^= 1;
+        }
+        if constexpr (kTiles == 2) {
+          ok = ok && wait(sh.k_full[k.i], k.phase);
+          if (!ok) break;
+          ptx::tc_fence_after();
+          for (int tt = 0; tt < nt; ++tt) scores(tt, 0);
+          commit(bar(sh.k_empty[k.i]));
+          k.next();
+          for (int j = 0; j < n && ok; ++j) {
+            const bool ahead = j + 1 < n;
+            ok = wait(sh.v_full[v.i], v.phase);
+            for (int tt = 0; tt < nt && ok; ++tt) {
+              for (int half = 0; half < 2 && ok; ++half) {
+                ok = wait(sh.p_full[tt][half], p_phase[tt][half]);
+                p_phase[tt][half] ^= 1;
+                if (!ok) break;
+                ptx::tc_fence_after();
+                values(tt, half * 32, half, j > 0 || half > 0);
+              }
               if (!ok) break;
-              ptx::tc_fence_after();
-              values(tt, half, j > 0 || half > 0);
+              commit(bar(sh.o_done[tt]));
+              // (before the wait for the next keys: unpacking them takes the ring along, and with it the next values)
+              if (tt == nt - 1) commit(bar(sh.v_empty[v.i]));
+              if (ahead) {  // S lies where P does: P has to be read first
+                if (tt == 0) ok = wait(sh.k_full[k.i], k.phase);
+                ok = ok && wait(sh.o_done[tt], o_phase[tt]);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                scores(tt, 0);
+              }
+              o_phase[tt] ^= 1;
             }
             if (!ok) break;
-            commit(bar(sh.o_done[tt]));
-            // (before the wait for the next keys: unpacking them takes the ring along, and with it the next values)
-            if (tt == kTiles - 1) commit(bar(sh.v_empty[v.i]));
-            if (ahead) {  // S lies where P does: P has to be read first
-              if (tt == 0) ok = wait(sh.k_full[k.i], k.phase);
-              ok = ok && wait(sh.o_done[tt], o_phase);
-              if (!ok) break;
-              ptx::tc_fence_after();
-              scores(tt);
+            v.next();
+            if (ahead) {
+              commit(bar(sh.k_empty[k.i]));
+              k.next();
             }
           }
-          if (!ok) break;
-          p_phase ^= 1;
-          o_phase ^= 1;
-          v.next();
-          if (ahead) {
-            commit(bar(sh.k_empty[k.i]));
-            k.next();
+        } else {
+          for (int j = 0; j < n + 2 && ok; ++j) {  // scores of unit j, product with the values of unit j - 2; both have the same buffer
+            if (j >= 2) {
+              ok = wait(sh.v_full[v.i], v.phase) && wait(sh.p_full[0][buf], p_phase[0][buf]);
+              p_phase[0][buf] ^= 1;
+              if (!ok) break;
+              ptx::tc_fence_after();
+              values(0, buf * kKeys, 0, j > 2);
+              commit(bar(sh.o_done[0]));
+              commit(bar(sh.v_empty[v.i]));  // (before the wait for the next keys, as above)
+              v.next();
+            }
+            if (j < n) {
+              ok = wait(sh.k_full[k.i], k.phase);
+              if (j >= 2) ok = ok && wait(sh.o_done[0], o_phase[0]);
+              if (!ok) break;
+              ptx::tc_fence_after();
+              scores(0, buf);
+              commit(bar(sh.k_empty[k.i]));
+              k.next();
+            }
+            if (j >= 2) o_phase[0] ^= 1;
+            buf ^= 1;
           }
+          // (two turns more than units: buf is the next unit's)
         }
         more = ok && at.next(p);
       }
     }
-  } else {
-    // ---- softmax ---------------------------------------------------------------------------------------
-    const int tt = warp >> 2, r128 = (warp & 3) * 32 + lane;
-    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t t_s = tmem + lanes + tt * 128, t_o = tmem + lanes + kTiles * 128 + tt * 128;
-    const float to_log2 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);
-    Turn<kSeenStages> seen;
-    uint32_t s_phase = 0, o_phase = 0;
-    bool more = true, ok = true;
-    while (more) {
-      // the row's query, its largest element in [2^15, 2^16), elements paired as the codes are
-      const int rows = kTopk ? p.group : at.r.n * p.group, r0 = at.rt * C::kRows + tt * kTileRows, r = r0 + r128;
-      int token = 0, head = 0;
-      float worth;
-      {
-        const uint32_t to = s_q + tt * C::kQueryBytes;
-        const uint4* src = nullptr;
-        if (r < rows) {
-          row_place(p, at.r.first, at.kvh, r, token, head);
-          src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + token * p.q_stride + static_cast<long long>(head) * D);
-        }
-        uint32_t top = 0;
-        if (src != nullptr) {
-#pragma unroll 4
-          for (int i = 0; i < D / 8; ++i) {
-            const uint4 x = __ldg(src + i);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
-          }
-        }
-        const int e = max(static_cast<int>(top >> 7), 21);
-        const float up = copysignf(__uint_as_float(static_cast<uint32_t>(127 + 127 + 15 - e) << 23), p.scale);
-        worth = fminf(__uint_as_float(static_cast<uint32_t>(e - 15) << 23) * to_log2, 0x1p80f);
-#pragma unroll 4
-        for (int i = 0; i < D / 8; ++i) {
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (src != nullptr) x = __ldg(src + i);
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-          float f[8];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            f[2 * j] = __uint_as_float(w[j] << 16) * up;
-            f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u) * up;
-          }
-          sts128(to + (i >> 3) * kHalfQ + swizzled(r128, i & 7), half2_bits(f[0], f[4]), half2_bits(f[1], f[5]), half2_bits(f[2], f[6]),
-                 half2_bits(f[3], f[7]));
-        }
-        ptx::fence_proxy_async();
-        ptx::tc_fence_before();  // (the item before has been read from tensor memory)
-        ptx::mbar_arrive(bar(sh.q_full[tt]));
-      }
-      // how far the row, and the tile's first row, see (dense form)
-      const long long limit = static_cast<long long>(at.r.ctx) + (r < rows ? r : rows - 1) / p.group;
-      const long long least = static_cast<long long>(at.r.ctx) + (r0 < rows ? r0 : rows - 1) / p.group;
-      float worth_bar = -INFINITY, shift = kNothing, l = 0.f;
-      const int unit0 = at.unit, unit1 = at.end();
-      for (int unit = unit0; unit < unit1 && ok; ++unit) {
-        ok = ptx::mbar_wait(bar(sh.seen_full[seen.i]), seen.phase, gave_up);
-        if (!__all_sync(0xffffffffu, ok)) {  // (a warp goes on, or gives up, as one)
-          ok = false;
-          break;
-        }
-        unsigned there[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) there[i] = sh.there[seen.i][i];
-        ptx::mbar_arrive(bar(sh.seen_empty[seen.i]));
-        seen.next();
-        const bool whole = (there[0] & there[1] & there[2] & there[3]) == 0xffffffffu &&
-                           (kTopk || static_cast<long long>(unit) * kKeys + kKeys - 1 <= least);
-        ok = ptx::mbar_wait(bar(sh.s_full[tt]), s_phase, gave_up);
-        s_phase ^= 1;
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          break;
-        }
-        ptx::tc_fence_after();
-        // column 8 m + i is key 8 m + (m + i) % 8
-        auto hide = [&](uint32_t (&v)[32], int chunk) {
-          const long long left = limit - (static_cast<long long>(unit) * kKeys + chunk * 32);
-          unsigned sees = chunk == 0 ? there[0] : chunk == 1 ? there[1] : chunk == 2 ? there[2] : there[3];
-          if constexpr (!kTopk) sees = left >= 31 ? sees : left < 0 ? 0u : sees & (0xffffffffu >> (31 - static_cast<int>(left)));
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const int m = i >> 3, key = m * 8 + ((m + (chunk & 1) * 4 + i) & 7);
-            if (!((sees >> key) & 1u)) v[i] = 0xff800000u;
-          }
-        };
-        float top = -INFINITY;
-#pragma unroll 1
-        for (int chunk = 0; chunk < 4; ++chunk) {
-          uint32_t v[32];
-          ptx::tmem_ld32(t_s + chunk * 32, v);
-          ptx::tmem_ld_wait(v);
-          if (!whole) hide(v, chunk);
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) top = fmaxf(fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), top);
-        }
-        const bool grows = top > worth_bar;
-        if (__any_sync(0xffffffffu, grows)) {
-          float back = 1.f;
-          if (grows) {
-            const float now = kPShift - top * worth;
-            back = ex2(now - shift);
-            worth_bar = top + kPSlack / worth;
-            shift = now;
-            l *= back;
-          }
-          if (unit > unit0) {  // what there is of O, once the product before is through
-            ok = ptx::mbar_wait(bar(sh.o_done[tt]), o_phase ^ 1, gave_up);
-            if (!__all_sync(0xffffffffu, ok)) {
-              ok = false;
-              break;
-            }
-            ptx::tc_fence_after();
-#pragma unroll 1
-            for (int chunk = 0; chunk < D / 32; ++chunk) {
-              uint32_t w[32];
-              ptx::tmem_ld32(t_o + chunk * 32, w);
-              ptx::tmem_ld_wait(w);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * back);
-              tmem_st32(t_o + chunk * 32, w);
-            }
-          }
-        }
-        float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll 1
-        for (int chunk = 0; chunk < 4; ++chunk) {
-          uint32_t v[32], h[16];
-          ptx::tmem_ld32(t_s + chunk * 32, v);
-          ptx::tmem_ld_wait(v);
-          if (!whole) hide(v, chunk);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float a = ex2(__fmaf_rn(__uint_as_float(v[2 * i]), worth, shift)), b = ex2(__fmaf_rn(__uint_as_float(v[2 * i + 1]), worth, shift));
-            sum0 += a;
-            sum1 += b;
-            h[i] = half2_bits(a, b);
-          }
-          tmem_st16(t_s + chunk * 16, h);
-          if (chunk & 1) {  // half of the keys: their product may begin
-            tmem_st_wait();
-            ptx::tc_fence_before();
-            ptx::mbar_arrive(bar(sh.p_full[tt][chunk >> 1]));
-          }
-        }
-        l += sum0 + sum1;
-        o_phase ^= 1;
-      }
-      if (!ok) break;
-      // the item's end, or the run's
-      ok = ptx::mbar_wait(bar(sh.o_done[tt]), o_phase ^ 1, gave_up);
-      if (!__all_sync(0xffffffffu, ok)) {
-        ok = false;
-        break;
-      }
-      ptx::tc_fence_after();
-      const bool begins = unit0 == 0, ends = unit1 == at.units;
-      const float m = l > 0.f ? kPShift - shift : -INFINITY;
-      float* part = sb.cta + (static_cast<long long>(blockIdx.x) * 2 + (begins ? 1 : 0)) * part_floats(C::kRows, D);
-      const int n = tt * kTileRows + r128;
-#pragma unroll 1
-      for (int chunk = 0; chunk < D / 32; ++chunk) {
-        uint32_t v[32];
-        ptx::tmem_ld32(t_o + chunk * 32, v);
-        ptx::tmem_ld_wait(v);
-        if (begins && ends) {
-          if (r < rows) {
-            const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
-            uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + (static_cast<long long>(token) * p.Hq + head) * D + chunk * 32);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t h[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                h[j] = bf162_bits(__uint_as_float(v[i * 8 + j * 2]) * inv, __uint_as_float(v[i * 8 + j * 2 + 1]) * inv);
-              to[i] = make_uint4(h[0], h[1], h[2], h[3]);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4*>(part + n * D + chunk * 32 + i * 4) = make_uint4(v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3]);
-        }
-      }
-      if (begins && ends) {
-        if (r < rows && p.lse != nullptr)
-          p.lse[static_cast<long long>(token) * p.Hq + head] = l > 0.f ? (m - kPShift + log2f(l)) * kLn2 : -INFINITY;
-      } else {
-        part[C::kRows * D + n] = m;
-        part[C::kRows * D + C::kRows + n] = l;
-        if (tid == 0)
-          sb.desc[blockIdx.x].part[begins ? 1 : 0] = PartDesc{at.b, at.kvh, at.rt, kValid | (begins ? kBegins : 0) | (ends ? kEnds : 0)};
-      }
-      more = at.next(p);
     }
   }
 
@@ -855,7 +1035,7 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
   if (warp == C::kMmaWarp) {
     // every product and every signal of theirs is through before the memory goes, also where a role gave up
     commit(bar(sh.drained));
-    ptx::mbar_wait(bar(sh.drained), 0, sh.drain_flag);
+    long_wait(bar(sh.drained), 0, sh.drain_flag);
     __syncwarp();
     ptx::tmem_dealloc(tmem, C::kTmemCols);
   }
