@@ -730,8 +730,7 @@ cudaError_t launch_rows(const Kv4AttnParams& p, void* scratch, Control* ctl, int
   sb.ctl = ctl;
   const cudaError_t r = launch_chained(attention_rows_kernel<D, NT, kTopk>, dim3(grid), dim3(S::kThreads), S::kSmem, stream, 1, p, sb);
   if (r != cudaSuccess) return r;
-  return launch_chained(attention_join_kernel<D, S::kRows, kTopk>, dim3(grid, (S::kRows * D / 4 + 255) / 256), dim3(256), 0, stream, 1, p,
-                        sb, grid, false);
+  return launch_join<D, S::kRows, kTopk>(p, sb, grid, false, stream);
 }
 
 }  // namespace

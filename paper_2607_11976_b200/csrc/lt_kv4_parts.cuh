@@ -146,63 +146,65 @@ struct SplitBuffers {
 // Floats of a part: o[kRows][D], m[kRows] (powers of two), l[kRows].
 __host__ __device__ constexpr int part_floats(int rows, int D) { return rows * (D + 2); }
 
-// Items that span CTAs: CTA c joins the one that begins in run c with the pieces of the runs behind it.
+// Items that span CTAs: the CTAs (c, *) join the one that begins in run c with the pieces of the runs behind it.  Items of few rows span
+// many CTAs: there the 8 warps of a CTA share out the pieces of 32 groups of 4 elements, 4 of them under way each, and are joined in
+// turn.  Items of many rows span few: there each warp has elements of its own, and a CTA several turns (a CTA for every 32 groups of
+// elements took 50 us to launch: 1024 x 2048 positions 323 instead of 270 us).
+constexpr int kJoinWarps = 8;
 template <int D, int kRows, bool kTopk>
-__global__ void __launch_bounds__(256) attention_join_kernel(const Kv4AttnParams p, const SplitBuffers sb, int n_ctas, bool keep_status) {
-  constexpr int kFloats = part_floats(kRows, D);
+__global__ void __launch_bounds__(kJoinWarps * 32) attention_join_kernel(const Kv4AttnParams p, const SplitBuffers sb, int n_ctas, bool keep_status) {
+  constexpr int kFloats = part_floats(kRows, D), kThreads = kJoinWarps * 32, kJoinGroups = kRows <= 16 ? kJoinWarps : 1;
+  __shared__ int s_status, s_end;
+  __shared__ float4 s_o[kJoinGroups][32];
+  __shared__ float s_m[kJoinGroups][32], s_l[kJoinGroups][32];
   chain_wait();
   if (blockIdx.x == 0 && blockIdx.y == 0) {  // the call's status: what its CTAs left
-    __shared__ int s_status;
     if (threadIdx.x == 0) s_status = keep_status ? sb.ctl->status : 0;
     __syncthreads();
-    for (int c = threadIdx.x; c < n_ctas; c += 256)
+    for (int c = threadIdx.x; c < n_ctas; c += kThreads)
       if (sb.desc[c].status != 0) atomicOr(&s_status, sb.desc[c].status);
     __syncthreads();
     if (threadIdx.x < sizeof(Control) / 4) reinterpret_cast<int*>(sb.ctl)[threadIdx.x] = threadIdx.x == 0 ? s_status : 0;
   }
   const PartDesc run = sb.desc[blockIdx.x].part[1];
   if (!(run.flags & kValid)) return;
-  // the CTAs behind this one that hold pieces of it: up to the first whose piece ends it
-  int n_more = 0;
-  for (int base = blockIdx.x + 1; base < n_ctas; base += 256) {
+  // up to the first CTA whose piece ends it (a run without units has no piece)
+  if (threadIdx.x == 0) s_end = n_ctas;
+  __syncthreads();
+  for (int base = blockIdx.x + 1; base < n_ctas; base += kThreads) {
     const int c = base + threadIdx.x;
-    const int flags = c < n_ctas ? sb.desc[c].part[0].flags : 0;
-    const bool ends = (flags & kEnds) != 0;
-    // (a run without units has no piece, and takes no part in the order)
-    __shared__ int s_end;
-    if (threadIdx.x == 0) s_end = n_ctas;
+    if (c < n_ctas && (sb.desc[c].part[0].flags & kEnds)) atomicMin(&s_end, c);
     __syncthreads();
-    if (ends) atomicMin(&s_end, c);
+    const int end = s_end;
     __syncthreads();
-    n_more = (s_end < n_ctas ? s_end + 1 : n_ctas) - (blockIdx.x + 1);
-    const bool found = s_end < n_ctas;
-    __syncthreads();
-    if (found) break;
+    if (end < n_ctas) break;
   }
+  const int n_more = (s_end < n_ctas ? s_end + 1 : n_ctas) - (blockIdx.x + 1);
   int first = run.b, rows = p.group;
   if constexpr (!kTopk) {
     const Kv4Request r = kv4_request(p, run.b);
     first = r.first;
     rows = r.n * p.group;
   }
-  for (int v = blockIdx.y * 256 + threadIdx.x; v < kRows * D / 4; v += gridDim.y * 256) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = kJoinGroups > 1 ? warp : 0;
+  constexpr int kPerCta = kJoinGroups > 1 ? 32 : kThreads;
+  for (int v = blockIdx.y * kPerCta + threadIdx.x % kPerCta; v < kRows * D / 4; v += gridDim.y * kPerCta) {
     const int n = v * 4 / D, d = v * 4 % D, r = run.rt * kRows + n;
-    if (r >= rows) continue;
-    const float* part = sb.cta + (static_cast<long long>(blockIdx.x) * 2 + 1) * kFloats;
-    float4 o = *reinterpret_cast<const float4*>(part + n * D + d);
-    float m = part[kRows * D + n], l = part[kRows * D + kRows + n];
-    constexpr int kAhead = 8;  // pieces under way at once
-    for (int c0 = 0; c0 < n_more; c0 += kAhead) {
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = -INFINITY, l = 0.f;
+    constexpr int kAhead = 4;  // pieces under way at once
+    // piece 0 is CTA c's own, piece i the one of CTA c + i
+    for (int i0 = group; i0 <= n_more; i0 += kAhead * kJoinGroups) {
       float4 x[kAhead];
       float pm[kAhead], pl[kAhead];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
+        const int at = i0 + i * kJoinGroups, c = blockIdx.x + at;
         x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         pm[i] = -INFINITY;
         pl[i] = 0.f;
-        const int c = blockIdx.x + 1 + c0 + i;
-        if (c0 + i < n_more && (sb.desc[c].part[0].flags & kValid)) {
-          part = sb.cta + static_cast<long long>(c) * 2 * kFloats;
+        if (at <= n_more && r < rows && (at == 0 || (sb.desc[c].part[0].flags & kValid))) {
+          const float* part = sb.cta + (static_cast<long long>(c) * 2 + (at == 0 ? 1 : 0)) * kFloats;
           x[i] = *reinterpret_cast<const float4*>(part + n * D + d);
           pm[i] = part[kRows * D + n];
           pl[i] = part[kRows * D + kRows + n];
@@ -211,10 +213,25 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const Kv4AttnParams
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) join(o, m, l, x[i], pm[i], pl[i]);
     }
+    if constexpr (kJoinGroups > 1) {  // (one turn only: the grid covers the item)
+      s_o[group][lane] = o;
+      s_m[group][lane] = m;
+      s_l[group][lane] = l;
+      __syncthreads();
+      if (group != 0) return;
+      const int groups = n_more + 1 < kJoinGroups ? n_more + 1 : kJoinGroups;
+      for (int g = 1; g < groups; ++g) join(o, m, l, s_o[g][lane], s_m[g][lane], s_l[g][lane]);
+    }
+    if (r >= rows) continue;
     int token, head;
     row_place(p, first, run.kvh, r, token, head);
     write_row4<D>(p, token, head, d, o, m, l);
   }
+}
+template <int D, int kRows, bool kTopk>
+inline cudaError_t launch_join(const Kv4AttnParams& p, const SplitBuffers& sb, int n_ctas, bool keep_status, cudaStream_t stream) {
+  return launch_chained(attention_join_kernel<D, kRows, kTopk>, dim3(n_ctas, kRows <= 16 ? kRows * D / 128 : 8), dim3(kJoinWarps * 32), 0, stream, 1,
+                        p, sb, n_ctas, keep_status);
 }
 
 }  // namespace

@@ -1056,8 +1056,7 @@ cudaError_t launch_tiles(const Kv4AttnParams& p, void* scratch, Control* ctl, in
   sb.ctl = ctl;
   const cudaError_t r = launch_chained(attention_tiles_kernel<D, kTiles, kTopk>, dim3(grid), dim3(C::kThreads), C::kSmem, stream, 1, p, sb);
   if (r != cudaSuccess) return r;
-  return launch_chained(attention_join_kernel<D, C::kRows, kTopk>, dim3(grid, (C::kRows * D / 4 + 255) / 256), dim3(256), 0, stream, 1, p, sb,
-                        grid, keep_status);
+  return launch_join<D, C::kRows, kTopk>(p, sb, grid, keep_status, stream);
 }
 
 }  // namespace
