@@ -29,7 +29,9 @@ __host__ __device__ constexpr int kv4_row_bytes(int D) { return D + D / 8; }
 
 // Scale of a group from its largest magnitude (both roundings to nearest even).
 __device__ __forceinline__ __half kv4_scale(float amax) {
-  const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(amax, 7.f)));
+  // amax / 7, correctly rounded: a product and its correction (an infinite amax stays as it is)
+  const float seventh = 1.f / 7.f, q = amax * seventh, r = __fmaf_rn(q, -7.f, amax);
+  const float s = __bfloat162float(__float2bfloat16_rn(amax < INFINITY ? __fmaf_rn(r, seventh, q) : amax));
   return __float2half_rn(fminf(s, kKvMaxScale));
 }
 

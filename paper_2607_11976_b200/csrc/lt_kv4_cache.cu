@@ -159,10 +159,28 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const TablePar
 
 // ---------------------------------------------------------------------------------------------
 // Writer.  A thread takes 8 consecutive elements (one or two 16-byte loads), four threads share a group: two shuffles give its largest
-// magnitude.  16 threads (D = 128) hold a head's keys and the 16 beside them its values, so a warp writes whole rows.  HBM bound:
-// it reads 2 Hkv D elements a token and writes 9 / 16 byte for each.
+// magnitude.  16 threads (D = 128) hold a head's keys and the 16 beside them its values, so a warp writes whole rows.  It reads
+// 2 Hkv D elements a token and writes 9 / 16 byte for each; with 16 instructions an element it was bound by those, not by HBM
+// (65,536 tokens of 8 heads: 200 us), so ordinary groups of bf16 take a shorter way of 6: the quotient by a reciprocal and one
+// correction, the nibble from the bits of a sum that rounds.
 // ---------------------------------------------------------------------------------------------
 constexpr int kCacheThreads = 256;
+constexpr int kCacheAhead = 4;  // loads in flight per thread
+
+// A thread's place in the row of (token, head) items, kept up by additions.
+struct ItemWalk {
+  long long t;
+  int h;
+  __device__ __forceinline__ ItemWalk(long long item, int heads) : t(item / heads), h(static_cast<int>(item - t * heads)) {}
+  __device__ __forceinline__ void add(long long dt, int dh, int heads) {
+    t += dt;
+    h += dh;
+    if (h >= heads) {
+      h -= heads;
+      ++t;
+    }
+  }
+};
 
 template <typename In>
 struct Vec8 {
@@ -185,6 +203,35 @@ __device__ __forceinline__ void unpack8(const Vec8<float>& v, float (&x)[8]) {
     x[4 * i + 3] = __uint_as_float(v.raw[i].w);
   }
 }
+// Largest magnitude's bits; a NaN counts above infinity here.
+__device__ __forceinline__ uint32_t top_bits(const Vec8<__nv_bfloat16>& v) {
+  const uint32_t k = 0x7fff7fffu;
+  const uint32_t m = __vmaxu2(__vmaxu2(v.raw[0].x & k, v.raw[0].y & k), __vmaxu2(v.raw[0].z & k, v.raw[0].w & k));
+  return max(m & 0xffffu, m >> 16) << 16;
+}
+__device__ __forceinline__ uint32_t top_bits(const Vec8<float>& v) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    m = max(m, max(max(v.raw[i].x & 0x7fffffffu, v.raw[i].y & 0x7fffffffu), max(v.raw[i].z & 0x7fffffffu, v.raw[i].w & 0x7fffffffu)));
+  return m;
+}
+
+// Eight codes of ordinary bf16 values: the scale is a normal fp16 number and not cut off at its maximum, so |x / s| < 7.1.  x and s have 8
+// significant bits: x / s is a tie between two integers exactly, or off by 2^-8 of itself or more.  q + (x - q s) inv is the quotient
+// rounded once, so a tie is met exactly; 1.5 * 2^23 + 8 + q then rounds to the nearest integer, ties to even, and has code = 8 + n in its
+// lowest bits.  The constant's bits, shifted along, sum up to another constant.
+__device__ __forceinline__ uint32_t ordinary_codes(const float (&x)[8], float s, float inv) {
+  uint32_t sum = 0;
+#pragma unroll
+  for (int i = 7; i >= 0; --i) {
+    const float q = x[i] * inv, exact = __fmaf_rn(__fmaf_rn(-q, s, x[i]), inv, q);
+    sum = (sum << 4) + __float_as_uint(exact + 12582920.f);
+  }
+  constexpr uint32_t kBits = 0x4B400000u;  // 1.5 * 2^23; its copies from the third on fall out at the top, but for their lowest bits
+  constexpr uint32_t kAll = kBits + (kBits << 4) + (kBits << 8) + (kBits << 12) + (kBits << 16) + (kBits << 20) + (kBits << 24) + (kBits << 28);
+  return sum - kAll;
+}
 
 struct AppendParams {
   const void* k;
@@ -199,53 +246,61 @@ struct AppendParams {
 template <typename In, int D>
 __global__ void __launch_bounds__(kCacheThreads) append_kernel(const AppendParams p) {
   chain_wait();
-  constexpr int kPer = D / 4;       // threads of one (token, head): keys and values, 8 elements each
-  constexpr int kRow = kv4_row_bytes(D);
-  const long long items = static_cast<long long>(p.T) * p.Hkv;
+  constexpr int kPer = D / 4;  // threads of one (token, head): keys and values, 8 elements each
+  constexpr int kRow = kv4_row_bytes(D), kItems = kCacheThreads / kPer;
   const int sub = threadIdx.x % kPer;
   const bool is_v = sub >= kPer / 2;
   const int e = (sub % (kPer / 2)) * 8;  // first element
-  constexpr int kAhead = 4;              // loads in flight per thread
-  const long long step = static_cast<long long>(gridDim.x) * (kCacheThreads / kPer);
-  // (whole warps stay in the loop: the shuffles below name all lanes)
-  const long long first = static_cast<long long>(blockIdx.x) * (kCacheThreads / kPer) + threadIdx.x / kPer;
-  for (long long base = first - threadIdx.x / kPer; base < items; base += step * kAhead) {
-    Vec8<In> x[kAhead];
-    long long slot[kAhead];
-    int head[kAhead];
+  const In* src = is_v ? static_cast<const In*>(p.v) : static_cast<const In*>(p.k);
+  const long long stride = is_v ? p.v_stride : p.k_stride;
+  const int step = gridDim.x * kItems, dt = step / p.Hkv, dh = step - dt * p.Hkv;
+  ItemWalk at(blockIdx.x * kItems + threadIdx.x / kPer, p.Hkv);
+  // (whole warps stay in the loop, the shuffles below name all lanes: it runs as long as the CTA's first item is there)
+  ItemWalk lead(blockIdx.x * kItems, p.Hkv);
+  while (lead.t < p.T) {
+    Vec8<In> x[kCacheAhead];
+    int slot[kCacheAhead], head[kCacheAhead];
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const long long item = base + a * step + threadIdx.x / kPer;
+    for (int a = 0; a < kCacheAhead; ++a) {
       slot[a] = -1;
-      head[a] = 0;
+      head[a] = at.h;
 #pragma unroll
       for (int i = 0; i < static_cast<int>(sizeof(In) / 2); ++i) x[a].raw[i] = make_uint4(0, 0, 0, 0);
-      if (item < items) {
-        const long long t = item / p.Hkv;
-        head[a] = static_cast<int>(item - t * p.Hkv);
-        slot[a] = p.slot_map[t];
-        const In* src = is_v ? static_cast<const In*>(p.v) + t * p.v_stride : static_cast<const In*>(p.k) + t * p.k_stride;
-        const uint4* at = reinterpret_cast<const uint4*>(src + head[a] * D + e);
+      if (at.t < p.T) {
+        slot[a] = p.slot_map[at.t];
+        const uint4* from = reinterpret_cast<const uint4*>(src + at.t * stride + at.h * D + e);
 #pragma unroll
-        for (int i = 0; i < static_cast<int>(sizeof(In) / 2); ++i) x[a].raw[i] = __ldg(at + i);
+        for (int i = 0; i < static_cast<int>(sizeof(In) / 2); ++i) x[a].raw[i] = __ldg(from + i);
       }
+      at.add(dt, dh, p.Hkv);
+      lead.add(dt, dh, p.Hkv);
     }
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
+    for (int a = 0; a < kCacheAhead; ++a) {
+      uint32_t top = top_bits(x[a]);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       float f[8];
       unpack8(x[a], f);
-      float amax = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(f[i]));
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-      const __half scale = kv4_scale(amax);
-      const float s = __half2float(scale), inv = s > 0.f ? 1.f / s : 0.f;
+      __half scale = kv4_scale(__uint_as_float(top));
+      const float s = __half2float(scale);
       uint32_t codes = 0;
+      if (sizeof(In) == 2 && top <= 0x46600000u && s >= 0x1p-14f) {  // (14336 = 7 * 2048)
+        codes = ordinary_codes(f, s, __fdividef(1.f, s));
+      } else {
+        float amax = 0.f;  // without the NaN
 #pragma unroll
-      for (int i = 0; i < 8; ++i) codes |= kv4_code(f[i], s, inv) << (4 * i);
+        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(f[i]));
+        const unsigned quad = 0xfu << (threadIdx.x & 28);  // (a group's four threads take the same way)
+        amax = fmaxf(amax, __shfl_xor_sync(quad, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(quad, amax, 2));
+        scale = kv4_scale(amax);
+        const float t = __half2float(scale), inv = t > 0.f ? 1.f / t : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) codes |= kv4_code(f[i], t, inv) << (4 * i);
+      }
       if (slot[a] < 0 || slot[a] >= p.pool_rows) continue;
-      uint8_t* row = p.pool + (((slot[a] / kPageKeys) * p.Hkv + head[a]) * kPageKeys + slot[a] % kPageKeys) * kRow;
+      uint8_t* row = p.pool + ((static_cast<long long>(slot[a] / kPageKeys) * p.Hkv + head[a]) * kPageKeys + slot[a] % kPageKeys) * kRow;
       *reinterpret_cast<uint32_t*>(row + sub * 4) = codes;
       if ((sub & 3) == 0) *reinterpret_cast<__half*>(row + D + (sub / 4) * 2) = scale;
     }
@@ -253,7 +308,8 @@ __global__ void __launch_bounds__(kCacheThreads) append_kernel(const AppendParam
 }
 
 // ---------------------------------------------------------------------------------------------
-// Reader: the values that the cache holds, in the caller's type (rounded once); zeros where there is no slot.
+// Reader: the values that the cache holds, in the caller's type (rounded once); zeros where there is no slot.  A code with a constant
+// or-ed into an exponent is 128 + u (bf16 pairs: one more subtraction and the product, exact up to its rounding) or 2^23 + u (fp32).
 // ---------------------------------------------------------------------------------------------
 struct ReadParams {
   const uint8_t* pool;
@@ -264,16 +320,27 @@ struct ReadParams {
   void* v_out;
 };
 
-__device__ __forceinline__ void store8(__nv_bfloat16* at, const float (&x)[8]) {
+__device__ __forceinline__ uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* at, uint32_t codes, __half scale) {
+  const uint32_t s = __bfloat16_as_ushort(__float2bfloat16_rn(__half2float(scale))), s2 = s | (s << 16);  // (8 bits: exact)
   uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  for (int i = 0; i < 4; ++i) {  // elements i and i + 4
+    const uint32_t v = bf16x2_fma(((codes >> (4 * i)) & 0x000F000Fu) | 0x43004300u, 0x3F803F80u, 0xC308C308u);  // 128 + u - 136
+    w[i] = bf16x2_fma(v, s2, 0x80008000u);                                                                     // v s - 0
   }
-  *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+  *reinterpret_cast<uint4*>(at) = make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[0], w[1], 0x7632),
+                                             __byte_perm(w[2], w[3], 0x7632));
 }
-__device__ __forceinline__ void store8(float* at, const float (&x)[8]) {
+__device__ __forceinline__ void store8(float* at, uint32_t codes, __half scale) {
+  const float s = __half2float(scale);
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (__uint_as_float(((codes >> (4 * i)) & 15u) | 0x4B000000u) - 8388616.f) * s;
   reinterpret_cast<float4*>(at)[0] = make_float4(x[0], x[1], x[2], x[3]);
   reinterpret_cast<float4*>(at)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
@@ -282,41 +349,38 @@ template <typename Out, int D>
 __global__ void __launch_bounds__(kCacheThreads) read_kernel(const ReadParams p) {
   chain_wait();
   constexpr int kPer = D / 4;
-  constexpr int kRow = kv4_row_bytes(D);
-  const long long items = static_cast<long long>(p.n) * p.Hkv;
+  constexpr int kRow = kv4_row_bytes(D), kItems = kCacheThreads / kPer;
   const int sub = threadIdx.x % kPer;
   const int e = (sub % (kPer / 2)) * 8;
   Out* out = static_cast<Out*>(sub >= kPer / 2 ? p.v_out : p.k_out);
-  constexpr int kAhead = 4;
-  const long long step = static_cast<long long>(gridDim.x) * (kCacheThreads / kPer);
-  for (long long base = static_cast<long long>(blockIdx.x) * (kCacheThreads / kPer) + threadIdx.x / kPer; base < items;
-       base += step * kAhead) {
-    uint32_t codes[kAhead];
-    __half scale[kAhead];
+  const int step = gridDim.x * kItems, dt = step / p.Hkv, dh = step - dt * p.Hkv;
+  ItemWalk at(blockIdx.x * kItems + threadIdx.x / kPer, p.Hkv);
+  while (at.t < p.n) {
+    uint32_t codes[kCacheAhead];
+    __half scale[kCacheAhead];
+    Out* to[kCacheAhead];
+    int slot[kCacheAhead];
+    ItemWalk place = at;
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const long long item = base + a * step;
+    for (int a = 0; a < kCacheAhead; ++a) {
+      slot[a] = place.t < p.n ? p.slots[place.t] : -1;
+      place.add(dt, dh, p.Hkv);
+    }
+#pragma unroll
+    for (int a = 0; a < kCacheAhead; ++a) {
       codes[a] = 0x88888888u;
       scale[a] = __ushort_as_half(0);
-      if (item < items) {
-        const long long t = item / p.Hkv, slot = p.slots[t];
-        if (slot >= 0 && slot < p.pool_rows) {
-          const uint8_t* row = p.pool + (((slot / kPageKeys) * p.Hkv + (item - t * p.Hkv)) * kPageKeys + slot % kPageKeys) * kRow;
-          codes[a] = *reinterpret_cast<const uint32_t*>(row + sub * 4);
-          scale[a] = *reinterpret_cast<const __half*>(row + D + (sub / 4) * 2);
-        }
+      to[a] = at.t < p.n ? out + (at.t * p.Hkv + at.h) * D + e : nullptr;
+      if (slot[a] >= 0 && slot[a] < p.pool_rows) {
+        const uint8_t* row = p.pool + ((static_cast<long long>(slot[a] / kPageKeys) * p.Hkv + at.h) * kPageKeys + slot[a] % kPageKeys) * kRow;
+        codes[a] = *reinterpret_cast<const uint32_t*>(row + sub * 4);
+        scale[a] = *reinterpret_cast<const __half*>(row + D + (sub / 4) * 2);
       }
+      at.add(dt, dh, p.Hkv);
     }
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const long long item = base + a * step;
-      if (item >= items) break;
-      const float s = __half2float(scale[a]);
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(static_cast<int>((codes[a] >> (4 * i)) & 15u) - 8) * s;
-      store8(out + item * D + e, x);
-    }
+    for (int a = 0; a < kCacheAhead; ++a)
+      if (to[a] != nullptr) store8(to[a], codes[a], scale[a]);
   }
 }
 
