@@ -307,25 +307,38 @@ def lt_dsa_union_mask(idx, N: int, group: int, union_pos, union_len, member_mask
 # serving step over a key-value cache held in 4 bits
 # ---------------------------------------------------------------------------------------------
 
+# (Calls of a decode step take a few microseconds on the GPU: what is asked of the tensors here is asked once.)
+_I32, _U8 = torch.int32, torch.uint8
+
+
+def _dense(t: torch.Tensor, dtype) -> int:
+    """Pointer of a dense CUDA tensor of the dtype."""
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous CUDA tensor of {dtype}")
+    return t.data_ptr()
+
+
 def _rows(t: torch.Tensor, dtype) -> tuple:
-    """(pointer, row stride in elements) of a [T, H, D] CUDA view whose heads are dense."""
-    want = (torch.float32,) if dtype_code(dtype) == LT_DTYPE_F32 else (torch.bfloat16,)
-    if t.dim() != 3 or not t.is_cuda or t.dtype not in want or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
-        raise ValueError("expected a [T, H, D] CUDA tensor of the call's dtype with dense heads")
-    return t.data_ptr(), int(t.stride(0)) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    """(pointer, T, H, D, row stride in elements) of a [T, H, D] CUDA view whose heads are dense."""
+    T, H, D = t.shape
+    row, head, one = t.stride()
+    if one != 1 or (head != D and H > 1) or not t.is_cuda or t.dtype is not dtype:
+        raise ValueError(f"expected a [T, H, D] CUDA tensor of {dtype} with dense heads")
+    return t.data_ptr(), T, H, D, row if T > 1 else H * D
 
 
-def _ints(*tensors) -> None:
-    for t in tensors:
-        if t is not None and t.dtype != torch.int32:
-            raise ValueError("expected int32 tensors")
+def _value_type(dtype) -> tuple:
+    """(the library's code, torch's type) of the values of a call."""
+    code = _DTYPE_CODES[dtype] if dtype in _DTYPE_CODES else int(dtype)
+    return code, torch.float32 if code == LT_DTYPE_F32 else torch.bfloat16
 
 
-def _pool_shape(pool: torch.Tensor) -> tuple:
-    """(pages, key-value heads, D) of a pool uint8 [pages, Hkv, 64, D + D / 8]."""
-    if pool.dim() != 4 or pool.dtype != torch.uint8 or pool.shape[2] != LT_PAGE_KEYS or pool.shape[3] % 9 != 0:
+def _pool(pool: torch.Tensor) -> tuple:
+    """(pointer, pages, key-value heads, D) of a pool uint8 [pages, Hkv, 64, D + D / 8]."""
+    pages, Hkv, keys, row = pool.shape
+    if keys != LT_PAGE_KEYS or row % 9 != 0:
         raise ValueError("expected a pool uint8 [pages, Hkv, 64, D + D / 8]")
-    return pool.shape[0], pool.shape[1], pool.shape[3] // 9 * 8
+    return _dense(pool, _U8), pages, Hkv, row // 9 * 8
 
 
 def lt_kv4_page_bytes(Hkv: int, D: int) -> int:
@@ -345,76 +358,88 @@ def lt_page_tables(context_len, new_len, free_pages, page_table, total_len, quer
     [n_free], page_table [B, max_pages] (in and out), total_len [B], query_start [B + 1], slot_map [T], position [T],
     status [8]."""
     B, T = context_len.numel(), slot_map.numel()
-    _ints(context_len, new_len, free_pages, page_table, total_len, query_start, slot_map, position, status)
-    if (new_len.numel() != B or page_table.dim() != 2 or page_table.shape[0] != B or total_len.numel() != B or
-            query_start.numel() != B + 1 or position.numel() != T or status.numel() < 8):
+    rows, max_pages = page_table.shape
+    if (rows != B or new_len.numel() != B or total_len.numel() != B or query_start.numel() != B + 1 or position.numel() != T or
+            status.numel() < 8):
         raise ValueError("the tables disagree on the number of requests or tokens")
     n_free = 0 if free_pages is None else free_pages.numel()
-    _check(load().lt_page_tables(_ptr(context_len), _ptr(new_len), _ptr(free_pages) if n_free else None, n_free, B,
-                                 page_table.shape[1], T, _ptr(page_table), _ptr(total_len), _ptr(query_start), _ptr(slot_map),
-                                 _ptr(position), _ptr(status), _stream(stream)), "lt_page_tables")
+    code = load().lt_page_tables(_dense(context_len, _I32), _dense(new_len, _I32), _dense(free_pages, _I32) if n_free else None,
+                                 n_free, B, max_pages, T, _dense(page_table, _I32), _dense(total_len, _I32),
+                                 _dense(query_start, _I32), _dense(slot_map, _I32), _dense(position, _I32), _dense(status, _I32),
+                                 _stream(stream))
+    if code:
+        _check(code, "lt_page_tables")
 
 
 def lt_kv4_append(dtype, k, v, slot_map, pool, stream=None) -> None:
     """Quantises k, v [T, Hkv, D] (rows may be strided) into the slots of the pool."""
-    pages, Hkv, D = _pool_shape(pool)
-    if k.shape != v.shape or tuple(k.shape[1:]) != (Hkv, D) or slot_map.numel() != k.shape[0]:
+    code, values = _value_type(dtype)
+    pool_ptr, pages, Hkv, D = _pool(pool)
+    k_ptr, T, H, d, k_row = _rows(k, values)
+    v_ptr, vT, vH, vd, v_row = _rows(v, values)
+    if vT != T or H != Hkv or vH != Hkv or d != D or vd != D or slot_map.numel() != T:
         raise ValueError("k, v, slot_map and pool disagree")
-    _ints(slot_map)
-    (kp, ks), (vp_, vs) = _rows(k, dtype), _rows(v, dtype)
-    _check(load().lt_kv4_append(dtype_code(dtype), kp, vp_, ks, vs, _ptr(slot_map), k.shape[0], Hkv, D, _ptr(pool), pages,
-                                _stream(stream)), "lt_kv4_append")
+    code = load().lt_kv4_append(code, k_ptr, v_ptr, k_row, v_row, _dense(slot_map, _I32), T, Hkv, D, pool_ptr, pages,
+                                _stream(stream))
+    if code:
+        _check(code, "lt_kv4_append")
 
 
 def lt_kv4_read(dtype, pool, slots, k_out, v_out, stream=None) -> None:
     """Values of the slots as k_out, v_out [n, Hkv, D]."""
-    pages, Hkv, D = _pool_shape(pool)
-    if k_out.shape != v_out.shape or tuple(k_out.shape) != (slots.numel(), Hkv, D):
+    code, values = _value_type(dtype)
+    pool_ptr, pages, Hkv, D = _pool(pool)
+    n = slots.numel()
+    shape = k_out.shape
+    if shape != (n, Hkv, D) or v_out.shape != shape:
         raise ValueError("slots, outputs and pool disagree")
-    _ints(slots)
-    _rows(k_out, dtype), _rows(v_out, dtype)
-    _check(load().lt_kv4_read(dtype_code(dtype), _ptr(pool), pages, _ptr(slots), slots.numel(), Hkv, D, _ptr(k_out),
-                              _ptr(v_out), _stream(stream)), "lt_kv4_read")
+    code = load().lt_kv4_read(code, pool_ptr, pages, _dense(slots, _I32), n, Hkv, D, _dense(k_out, values), _dense(v_out, values),
+                              _stream(stream))
+    if code:
+        _check(code, "lt_kv4_read")
 
 
 def lt_kv4_attention_workspace_bytes(dtype, T: int, B: int, Hq: int, Hkv: int, D: int) -> int:
     return int(load().lt_kv4_attention_workspace_bytes(dtype_code(dtype), T, B, Hq, Hkv, D))
 
 
-def _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse):
-    pages, Hkv, D = _pool_shape(pool)
-    T, Hq = q.shape[0], q.shape[1]
+def _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse, workspace):
+    """The arguments of both forms: (dtype .. context_len), (B, T, Hq, Hkv, D), (out, lse), (workspace, bytes)."""
+    code, values = _value_type(dtype)
+    pool_ptr, pages, Hkv, D = _pool(pool)
+    q_ptr, T, Hq, d, q_row = _rows(q, values)
     B = context_len.numel()
-    if (q.dim() != 3 or q.shape[2] != D or out.shape != q.shape or out.dtype != q.dtype or page_table.dim() != 2 or
-            page_table.shape[0] != B or query_start.numel() != B + 1 or
-            (out_lse is not None and (out_lse.numel() != T * Hq or out_lse.dtype != torch.float32))):
+    rows, max_pages = page_table.shape
+    if (d != D or rows != B or out.shape != q.shape or query_start.numel() != B + 1 or
+            (out_lse is not None and out_lse.numel() != T * Hq)):
         raise ValueError("q, pool, tables and outputs disagree")
-    _ints(page_table, query_start, context_len)
-    qp, qs = _rows(q, dtype)
-    return pages, Hkv, D, T, Hq, B, qp, qs
+    return ((code, q_ptr, q_row, pool_ptr, pages, _dense(page_table, _I32), max_pages, _dense(query_start, _I32),
+             _dense(context_len, _I32)), (B, T, Hq, Hkv, D),
+            (_dense(out, values), None if out_lse is None else _dense(out_lse, torch.float32)),
+            (_ptr(workspace), workspace.numel() * workspace.element_size()))
 
 
 def lt_kv4_attention(dtype, q, pool, page_table, query_start, context_len, scale: float, out, out_lse, workspace,
                      max_new: int = 0, tunables: Optional[Tunables] = None, stream=None) -> None:
     """Causal attention of q [T, Hq, D] over the requests' pages (out [T, Hq, D], out_lse fp32 [T, Hq] or None)."""
-    pages, Hkv, D, T, Hq, B, qp, qs = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse)
-    _check(load().lt_kv4_attention(dtype_code(dtype), qp, qs, _ptr(pool), pages, _ptr(page_table), page_table.shape[1],
-                                   _ptr(query_start), _ptr(context_len), B, T, Hq, Hkv, D, max_new, scale, _ptr(out),
-                                   _ptr(out_lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                   ctypes.byref(tunables) if tunables else None, _stream(stream)), "lt_kv4_attention")
+    inputs, sizes, outputs, scratch = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse, workspace)
+    code = load().lt_kv4_attention(*inputs, *sizes, max_new, scale, *outputs, *scratch,
+                                   ctypes.byref(tunables) if tunables else None, _stream(stream))
+    if code:
+        _check(code, "lt_kv4_attention")
 
 
 def lt_kv4_attention_topk(dtype, q, pool, page_table, query_start, context_len, idx, scale: float, out, out_lse, workspace,
                           tunables: Optional[Tunables] = None, stream=None) -> None:
     """The same over the positions idx [T, topk] (int32, as lt_indexer_topk_paged writes them)."""
-    pages, Hkv, D, T, Hq, B, qp, qs = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse)
-    if idx.dim() != 2 or idx.shape[0] != T:
+    inputs, sizes, outputs, scratch = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse, workspace)
+    T, topk = idx.shape
+    if T != sizes[1]:
         raise ValueError("expected idx [T, topk]")
-    _ints(idx)
-    _check(load().lt_kv4_attention_topk(dtype_code(dtype), qp, qs, _ptr(pool), pages, _ptr(page_table), page_table.shape[1],
-                                        _ptr(query_start), _ptr(context_len), _ptr(idx), idx.shape[1], B, T, Hq, Hkv, D, scale,
-                                        _ptr(out), _ptr(out_lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                        ctypes.byref(tunables) if tunables else None, _stream(stream)), "lt_kv4_attention_topk")
+    code = load().lt_kv4_attention_topk(*inputs, _dense(idx, _I32), topk, *sizes, scale, *outputs, *scratch,
+                                        ctypes.byref(tunables) if tunables else None, _stream(stream))
+    if code:
+        _check(code, "lt_kv4_attention_topk")
 
 
 def lt_indexer_scores(dtype, q, w, k, k_scale, causal_offset: int, row_begin: int, row_end: int, out_scores,
