@@ -211,6 +211,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
   int req_b = 0, req_token = -1;
   Kv4Request req{0, 0, 0};
 
+  const int row3 = lane / 9, piece_at = (lane - row3 * 9) * (S::kRow / 9), piece3 = row3 * S::kRow + piece_at;
   auto load_indices = [&]() {
     idx_far = -1;
     if (idx_loaded < hi) {
@@ -274,18 +275,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
       const uint32_t dst = ring_addr + fetch_stage * S::kUnitBytes;
       if constexpr (kTopk) {
         const bool sees = near_page >= 0 && near_page < p.pool_pages;
-        const unsigned seen = __ballot_sync(0xffffffffu, sees);
-        seen_of[S::kStages - 1] = seen;
-        const int slot = sees ? near_page * kPageKeys + near_pos % kPageKeys : -1;
-        const uint8_t* head = p.pool + static_cast<long long>(ahead.kvh) * kPageKeys * S::kRow;
-        constexpr int kPiece = S::kRow % 16 == 0 ? 16 : 8, kPieces = S::kRow / kPiece;
+        seen_of[S::kStages - 1] = __ballot_sync(0xffffffffu, sees);
+        const uint8_t* mine = sees ? p.pool + near_page * page_bytes + (ahead.kvh * kPageKeys + (near_pos & (kPageKeys - 1))) * S::kRow : nullptr;
+        // 27 lanes take the 9 pieces of three rows at a time
+        constexpr int kPiece = S::kRow / 9;
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-          const int n = i * 32 + lane, key = n / kPieces, part = n - key * kPieces;
-          const int s = __shfl_sync(0xffffffffu, slot, key);
-          if (s >= 0)
-            cp_async<kPiece>(dst + key * S::kRow + part * kPiece,
-                             head + static_cast<long long>(s / kPageKeys) * page_bytes + (s % kPageKeys) * S::kRow + part * kPiece);
+        for (int j = 0; j < (kUnit + 2) / 3; ++j) {
+          const int key = j * 3 + row3;
+          const unsigned long long row = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), key & 31);
+          if (row != 0 && (j < kUnit / 3 ? row3 < 3 : row3 < kUnit % 3))
+            cp_async<kPiece>(dst + piece3 + j * 3 * S::kRow, reinterpret_cast<const uint8_t*>(row) + piece_at);
         }
         step_pages();
         load_indices();
