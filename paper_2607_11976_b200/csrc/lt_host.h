@@ -318,7 +318,7 @@ size_t kv4_tiles_scratch_bytes(int D);
 cudaError_t launch_kv4_attention_tiles(int D, bool pairs, const Kv4AttnParams& p, void* scratch, Control* ctl, int sms, bool keep_status,
                                        cudaStream_t stream);
 // lt_kv4_generic.cu
-// One CTA per (token, query head), any head count, fp32 arithmetic throughout.
+// fp32 arithmetic throughout, any head count.
 cudaError_t launch_kv4_attention_generic(int dtype, int D, const Kv4AttnParams& p, cudaStream_t stream);
 
 }  // namespace lt
