@@ -45,7 +45,7 @@ struct Cfg {
 };
 
 struct Shared {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_done[2], q_full[2], ring_full[6], ring_empty[6],
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_done[2][2], q_full[2], ring_full[6], ring_empty[6],
       seen_full[kSeenStages], seen_empty[kSeenStages], drained;
   unsigned there[kSeenStages][4];  // a bit per key of the tile
   int abort_flag[2], drain_flag[2];  // [1]: limit of a wait in microseconds (lt_ptx.cuh)
@@ -348,8 +348,8 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
       for (int j = 0; j < 2; ++j) {
         ptx::mbar_init(bar(sh.s_full[i][j]), 1);
         ptx::mbar_init(bar(sh.p_full[i][j]), kTileRows);
+        ptx::mbar_init(bar(sh.o_done[i][j]), 1);
       }
-      ptx::mbar_init(bar(sh.o_done[i]), 1);
       ptx::mbar_init(bar(sh.q_full[i]), kTileRows);
     }
     for (int i = 0; i < C::kRing; ++i) {
@@ -481,7 +481,7 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
     const uint32_t t_s = tmem + lanes + tt * 128, t_o = tmem + lanes + kTiles * 128 + tt * 128;
     const float to_log2 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);
     Turn<kSeenStages> seen;
-    uint32_t s_phase[2] = {0, 0}, o_phase = 0;
+    uint32_t s_phase[2] = {0, 0}, o_uses[2] = {0, 0};  // (o_uses: parity of the products that were asked for from a buffer)
     int buf = 0;
     bool more = true, ok = true;
     while (more) {
@@ -560,8 +560,8 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
         if (!warp_there) {
           ptx::mbar_arrive(bar(sh.p_full[tt][buf]));
           if (C::kBufs == 1) ptx::mbar_arrive(bar(sh.p_full[tt][1]));
+          o_uses[buf] ^= 1;
           if (C::kBufs == 2) buf ^= 1;
-          o_phase ^= 1;
           continue;
         }
         ptx::tc_fence_after();
@@ -620,7 +620,8 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
             l *= back;
           }
           if (unit > unit0) {  // what there is of O, once the product before is through
-            ok = long_wait(bar(sh.o_done[tt]), o_phase ^ 1, gave_up);
+            const int before = C::kBufs == 2 ? buf ^ 1 : 0;
+            ok = long_wait(bar(sh.o_done[tt][before]), o_uses[before] ^ 1, gave_up);
             if (!__all_sync(0xffffffffu, ok)) {
               ok = false;
               break;
@@ -672,12 +673,13 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
         float sum0, sum1;
         unpack2(sum, sum0, sum1);
         l += sum0 + sum1;
+        o_uses[buf] ^= 1;
         if (C::kBufs == 2) buf ^= 1;
-        o_phase ^= 1;
       }
       if (!ok) break;
       // the item's end, or the run's
-      if (tile_there) ok = long_wait(bar(sh.o_done[tt]), o_phase ^ 1, gave_up);
+      if (tile_there)
+        for (int i = 0; i < C::kBufs; ++i) ok = ok && long_wait(bar(sh.o_done[tt][i]), o_uses[i] ^ 1, gave_up);
       if (!__all_sync(0xffffffffu, ok)) {
         ok = false;
         break;
@@ -936,7 +938,7 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
     // ---- products --------------------------------------------------------------------------------------
     {
       Turn<C::kStages> k, v;
-      uint32_t q_phase[2] = {0, 0}, o_phase[2] = {0, 0}, p_phase[2][2] = {{0, 0}, {0, 0}};
+      uint32_t q_phase[2] = {0, 0}, o_phase[2][2] = {{0, 0}, {0, 0}}, p_phase[2][2] = {{0, 0}, {0, 0}};
       auto wait = [&](uint64_t& b, uint32_t phase) { return __all_sync(0xffffffffu, long_wait(bar(b), phase, gave_up)) != 0; };
       auto scores = [&](int tt, int buf) {
 #pragma unroll
@@ -980,17 +982,17 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
                 values(tt, half * 32, half, j > 0 || half > 0);
               }
               if (!ok) break;
-              commit(bar(sh.o_done[tt]));
+              commit(bar(sh.o_done[tt][0]));
               // (before the wait for the next keys: unpacking them takes the ring along, and with it the next values)
               if (tt == nt - 1) commit(bar(sh.v_empty[v.i]));
               if (ahead) {  // S lies where P does: P has to be read first
                 if (tt == 0) ok = wait(sh.k_full[k.i], k.phase);
-                ok = ok && wait(sh.o_done[tt], o_phase[tt]);
+                ok = ok && wait(sh.o_done[tt][0], o_phase[tt][0]);
                 if (!ok) break;
                 ptx::tc_fence_after();
                 scores(tt, 0);
               }
-              o_phase[tt] ^= 1;
+              o_phase[tt][0] ^= 1;
             }
             if (!ok) break;
             v.next();
@@ -1007,20 +1009,20 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
               if (!ok) break;
               ptx::tc_fence_after();
               values(0, buf * kKeys, 0, j > 2);
-              commit(bar(sh.o_done[0]));
+              commit(bar(sh.o_done[0][buf]));
               commit(bar(sh.v_empty[v.i]));  // (before the wait for the next keys, as above)
               v.next();
             }
             if (j < n) {
               ok = wait(sh.k_full[k.i], k.phase);
-              if (j >= 2) ok = ok && wait(sh.o_done[0], o_phase[0]);
+              if (j >= 2) ok = ok && wait(sh.o_done[0][buf], o_phase[0][buf]);
               if (!ok) break;
               ptx::tc_fence_after();
               scores(0, buf);
               commit(bar(sh.k_empty[k.i]));
               k.next();
             }
-            if (j >= 2) o_phase[0] ^= 1;
+            if (j >= 2) o_phase[0][buf] ^= 1;
             buf ^= 1;
           }
           // (two turns more than units: buf is the next unit's)

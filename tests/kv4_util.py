@@ -91,9 +91,45 @@ class Step:
         else:
             lt.lt_kv4_attention_topk(self.dtype, q, g["pool"], g["table"], g["start"], g["ctx"], on_gpu(idx), self.scale, out, lse, ws, tun)
         torch.cuda.synchronize()
+        assert lt.lt_read_status(ws) == [0] * 8, "a wait ran out or an index check failed"
         return out.double().cpu().numpy(), None if lse is None else lse.double().cpu().numpy()
 
-    def check(self, out, lse, idx=None, fused=True, n_most=None):
+    def reference_on_gpu(self, idx=None):
+        """kv4.attention(...) with torch's 64-bit operations, for sizes that the CPU would take minutes for."""
+        T, Hq, D, Hkv = self.T, self.Hq, self.D, self.Hkv
+        group = Hq // Hkv
+        kv = [on_gpu(x) for x in kv4.unpack_rows(self.clean)]  # [pages, Hkv, 64, D] each
+        q = on_gpu(self.q)
+        out, spread = (torch.full((T, Hq, D), float("nan"), dtype=torch.float64, device="cuda") for _ in range(2))
+        mass, lse = torch.zeros_like(out), torch.full((T, Hq), float("nan"), dtype=torch.float64, device="cuda")
+        weight = torch.zeros_like(lse)
+        for b in range(self.ctx.size):
+            t0, t1, ctx = int(self.start[b]), int(self.start[b + 1]), int(self.ctx[b])
+            if t1 == t0:
+                continue
+            at = torch.arange(ctx + t1 - t0, device="cuda")
+            page = on_gpu(self.table[b].astype(np.int64))[at // 64]
+            last = ctx + torch.arange(t1 - t0, device="cuda")
+            if idx is not None:
+                i = on_gpu(idx[t0:t1].astype(np.int64))
+                ok = (i >= 0) & (i <= last[:, None])
+                count = torch.zeros(t1 - t0, at.numel(), dtype=torch.float64, device="cuda")
+                count.scatter_add_(1, torch.where(ok, i, 0), ok.double())
+            else:
+                count = (at[None] <= last[:, None]).double()
+            for h in range(Hkv):
+                k, v = (x[page, h, at % 64] for x in kv)
+                hs = slice(h * group, (h + 1) * group)
+                x = q[t0:t1, hs]
+                s = self.scale * torch.einsum("tgd,nd->tgn", x, k) + torch.log(count)[:, None]
+                lse[t0:t1, hs] = torch.logsumexp(s, -1)
+                p = torch.exp(s - lse[t0:t1, hs, None]).nan_to_num(0.0)
+                out[t0:t1, hs], spread[t0:t1, hs] = p @ v, p @ v.abs()
+                mass[t0:t1, hs] = (count @ v.abs())[:, None]
+                weight[t0:t1, hs] = (abs(self.scale) * torch.einsum("tgd,nd->tgn", x.abs(), k.abs()) * (count > 0)[:, None]).amax(-1)
+        return [x.cpu().numpy() for x in (out, lse, spread, weight, mass)]
+
+    def check(self, out, lse, idx=None, fused=True, n_most=None, on_gpu_too=False):
         """Against the 64-bit definition, within what the roundings on the way can do.
 
         Fused path.  A score is a sum of exact products accumulated in fp32 over codes offset by 8 (u, begun at -8 sum q):
@@ -108,7 +144,10 @@ class Step:
         mass = sum |v|; the largest probability is at most the sum).
         The result is rounded to bf16 (2^-8 of itself).
         fp32 path: ds = weight * (D + 8) 2^-24, sums of n terms, and a result rounded to 2^-24."""
-        ref, ref_lse, spread, weight, mass = kv4.attention(self.q, self.pool, self.table, self.start, self.ctx, self.scale, idx)
+        if on_gpu_too:
+            ref, ref_lse, spread, weight, mass = self.reference_on_gpu(idx)
+        else:
+            ref, ref_lse, spread, weight, mass = kv4.attention(self.q, self.pool, self.table, self.start, self.ctx, self.scale, idx)
         end = int(self.start[-1])
         assert np.array_equal(out[end:], np.full_like(out[end:], 7.0)), "rows behind the last request were written"
         if fused:
