@@ -295,7 +295,8 @@ int lt_dsa_union_mask(const int32_t* idx, int T, int topk, int N, int group,
  * Requests.  B of them in consecutive rows of the step's batch: request b has rows query_start[b] .. query_start[b + 1] - 1
  * (ascending), and row query_start[b] + j stands at position context_len[b] + j.  Rows from query_start[B] on are padding:
  * no output is written there.  Positions 64 j .. 64 j + 63 of request b lie in page page_table[b][j].  A position whose table
- * entry is no page of the pool, or lies beyond the table, is seen by no token.
+ * entry is no page of the pool, or lies beyond the table, is seen by no token.  Limits: B <= 2^20, T <= 2^24, max_pages <= 2^24,
+ * Hkv <= 1024, fewer than 2^31 rows in the pool.
  * ---------------------------------------------------------------------------------------------
  */
 #define LT_KV4_GROUP 32
@@ -353,7 +354,7 @@ int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t
  *                 launched: any value is safe, a right one is fastest
  *   scale         any finite number
  *   workspace     device, 256-byte aligned, at least lt_kv4_attention_workspace_bytes(...) bytes, scratch; one per stream
- *   tunables      path (AUTO, FUSED, GENERIC), grid and wait_limit_us are used; NULL = defaults
+ *   tunables      path (AUTO, FUSED, GENERIC), grid (SMs to use) and wait_limit_us are used; NULL = defaults
  * q, and the keys and values of positions that some token sees, must be finite; what lies anywhere else in the pool is not
  * used, whatever it is.  Probabilities are rounded to fp16 for the products with the values, everything else is held in fp32;
  * results do not depend on the run (no atomics), but their last bits may on the lengths of the other requests of the batch.

@@ -311,19 +311,24 @@ def lt_dsa_union_mask(idx, N: int, group: int, union_pos, union_len, member_mask
 _I32, _U8 = torch.int32, torch.uint8
 
 
-def _dense(t: torch.Tensor, dtype) -> int:
-    """Pointer of a dense CUDA tensor of the dtype."""
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"expected a contiguous CUDA tensor of {dtype}")
+def _device() -> int:
+    """The current CUDA device, where the library launches (-2 before there is any)."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+
+
+def _dense(t: torch.Tensor, dtype, dev: int) -> int:
+    """Pointer of a dense tensor of the dtype on the current device."""
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous tensor of {dtype} on the current CUDA device")
     return t.data_ptr()
 
 
-def _rows(t: torch.Tensor, dtype) -> tuple:
-    """(pointer, T, H, D, row stride in elements) of a [T, H, D] CUDA view whose heads are dense."""
+def _rows(t: torch.Tensor, dtype, dev: int) -> tuple:
+    """(pointer, T, H, D, row stride in elements) of a [T, H, D] view whose heads are dense."""
     T, H, D = t.shape
     row, head, one = t.stride()
-    if one != 1 or (head != D and H > 1) or not t.is_cuda or t.dtype is not dtype:
-        raise ValueError(f"expected a [T, H, D] CUDA tensor of {dtype} with dense heads")
+    if one != 1 or (head != D and H > 1) or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"expected a [T, H, D] tensor of {dtype} with dense heads on the current CUDA device")
     return t.data_ptr(), T, H, D, row if T > 1 else H * D
 
 
@@ -333,12 +338,12 @@ def _value_type(dtype) -> tuple:
     return code, torch.float32 if code == LT_DTYPE_F32 else torch.bfloat16
 
 
-def _pool(pool: torch.Tensor) -> tuple:
+def _pool(pool: torch.Tensor, dev: int) -> tuple:
     """(pointer, pages, key-value heads, D) of a pool uint8 [pages, Hkv, 64, D + D / 8]."""
     pages, Hkv, keys, row = pool.shape
     if keys != LT_PAGE_KEYS or row % 9 != 0:
         raise ValueError("expected a pool uint8 [pages, Hkv, 64, D + D / 8]")
-    return _dense(pool, _U8), pages, Hkv, row // 9 * 8
+    return _dense(pool, _U8, dev), pages, Hkv, row // 9 * 8
 
 
 def lt_kv4_page_bytes(Hkv: int, D: int) -> int:
@@ -357,15 +362,15 @@ def lt_page_tables(context_len, new_len, free_pages, page_table, total_len, quer
     """Block tables, slot map and positions of a step: int32 CUDA tensors context_len [B], new_len [B], free_pages
     [n_free], page_table [B, max_pages] (in and out), total_len [B], query_start [B + 1], slot_map [T], position [T],
     status [8]."""
-    B, T = context_len.numel(), slot_map.numel()
+    dev, B, T = _device(), context_len.numel(), slot_map.numel()
     rows, max_pages = page_table.shape
     if (rows != B or new_len.numel() != B or total_len.numel() != B or query_start.numel() != B + 1 or position.numel() != T or
             status.numel() < 8):
         raise ValueError("the tables disagree on the number of requests or tokens")
     n_free = 0 if free_pages is None else free_pages.numel()
-    code = load().lt_page_tables(_dense(context_len, _I32), _dense(new_len, _I32), _dense(free_pages, _I32) if n_free else None,
-                                 n_free, B, max_pages, T, _dense(page_table, _I32), _dense(total_len, _I32),
-                                 _dense(query_start, _I32), _dense(slot_map, _I32), _dense(position, _I32), _dense(status, _I32),
+    code = load().lt_page_tables(_dense(context_len, _I32, dev), _dense(new_len, _I32, dev), _dense(free_pages, _I32, dev) if n_free else None,
+                                 n_free, B, max_pages, T, _dense(page_table, _I32, dev), _dense(total_len, _I32, dev),
+                                 _dense(query_start, _I32, dev), _dense(slot_map, _I32, dev), _dense(position, _I32, dev), _dense(status, _I32, dev),
                                  _stream(stream))
     if code:
         _check(code, "lt_page_tables")
@@ -373,13 +378,14 @@ def lt_page_tables(context_len, new_len, free_pages, page_table, total_len, quer
 
 def lt_kv4_append(dtype, k, v, slot_map, pool, stream=None) -> None:
     """Quantises k, v [T, Hkv, D] (rows may be strided) into the slots of the pool."""
+    dev = _device()
     code, values = _value_type(dtype)
-    pool_ptr, pages, Hkv, D = _pool(pool)
-    k_ptr, T, H, d, k_row = _rows(k, values)
-    v_ptr, vT, vH, vd, v_row = _rows(v, values)
+    pool_ptr, pages, Hkv, D = _pool(pool, dev)
+    k_ptr, T, H, d, k_row = _rows(k, values, dev)
+    v_ptr, vT, vH, vd, v_row = _rows(v, values, dev)
     if vT != T or H != Hkv or vH != Hkv or d != D or vd != D or slot_map.numel() != T:
         raise ValueError("k, v, slot_map and pool disagree")
-    code = load().lt_kv4_append(code, k_ptr, v_ptr, k_row, v_row, _dense(slot_map, _I32), T, Hkv, D, pool_ptr, pages,
+    code = load().lt_kv4_append(code, k_ptr, v_ptr, k_row, v_row, _dense(slot_map, _I32, dev), T, Hkv, D, pool_ptr, pages,
                                 _stream(stream))
     if code:
         _check(code, "lt_kv4_append")
@@ -387,13 +393,14 @@ def lt_kv4_append(dtype, k, v, slot_map, pool, stream=None) -> None:
 
 def lt_kv4_read(dtype, pool, slots, k_out, v_out, stream=None) -> None:
     """Values of the slots as k_out, v_out [n, Hkv, D]."""
+    dev = _device()
     code, values = _value_type(dtype)
-    pool_ptr, pages, Hkv, D = _pool(pool)
+    pool_ptr, pages, Hkv, D = _pool(pool, dev)
     n = slots.numel()
     shape = k_out.shape
     if shape != (n, Hkv, D) or v_out.shape != shape:
         raise ValueError("slots, outputs and pool disagree")
-    code = load().lt_kv4_read(code, pool_ptr, pages, _dense(slots, _I32), n, Hkv, D, _dense(k_out, values), _dense(v_out, values),
+    code = load().lt_kv4_read(code, pool_ptr, pages, _dense(slots, _I32, dev), n, Hkv, D, _dense(k_out, values, dev), _dense(v_out, values, dev),
                               _stream(stream))
     if code:
         _check(code, "lt_kv4_read")
@@ -404,25 +411,26 @@ def lt_kv4_attention_workspace_bytes(dtype, T: int, B: int, Hq: int, Hkv: int, D
 
 
 def _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse, workspace):
-    """The arguments of both forms: (dtype .. context_len), (B, T, Hq, Hkv, D), (out, lse), (workspace, bytes)."""
+    """The arguments of both forms: (dtype .. context_len), (B, T, Hq, Hkv, D), (out, lse), (workspace, bytes), device."""
+    dev = _device()
     code, values = _value_type(dtype)
-    pool_ptr, pages, Hkv, D = _pool(pool)
-    q_ptr, T, Hq, d, q_row = _rows(q, values)
+    pool_ptr, pages, Hkv, D = _pool(pool, dev)
+    q_ptr, T, Hq, d, q_row = _rows(q, values, dev)
     B = context_len.numel()
     rows, max_pages = page_table.shape
     if (d != D or rows != B or out.shape != q.shape or query_start.numel() != B + 1 or
             (out_lse is not None and out_lse.numel() != T * Hq)):
         raise ValueError("q, pool, tables and outputs disagree")
-    return ((code, q_ptr, q_row, pool_ptr, pages, _dense(page_table, _I32), max_pages, _dense(query_start, _I32),
-             _dense(context_len, _I32)), (B, T, Hq, Hkv, D),
-            (_dense(out, values), None if out_lse is None else _dense(out_lse, torch.float32)),
-            (_ptr(workspace), workspace.numel() * workspace.element_size()))
+    return ((code, q_ptr, q_row, pool_ptr, pages, _dense(page_table, _I32, dev), max_pages, _dense(query_start, _I32, dev),
+             _dense(context_len, _I32, dev)), (B, T, Hq, Hkv, D),
+            (_dense(out, values, dev), None if out_lse is None else _dense(out_lse, torch.float32, dev)),
+            (_dense(workspace, _U8, dev), workspace.numel()), dev)
 
 
 def lt_kv4_attention(dtype, q, pool, page_table, query_start, context_len, scale: float, out, out_lse, workspace,
                      max_new: int = 0, tunables: Optional[Tunables] = None, stream=None) -> None:
     """Causal attention of q [T, Hq, D] over the requests' pages (out [T, Hq, D], out_lse fp32 [T, Hq] or None)."""
-    inputs, sizes, outputs, scratch = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse, workspace)
+    inputs, sizes, outputs, scratch, _ = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse, workspace)
     code = load().lt_kv4_attention(*inputs, *sizes, max_new, scale, *outputs, *scratch,
                                    ctypes.byref(tunables) if tunables else None, _stream(stream))
     if code:
@@ -432,11 +440,11 @@ def lt_kv4_attention(dtype, q, pool, page_table, query_start, context_len, scale
 def lt_kv4_attention_topk(dtype, q, pool, page_table, query_start, context_len, idx, scale: float, out, out_lse, workspace,
                           tunables: Optional[Tunables] = None, stream=None) -> None:
     """The same over the positions idx [T, topk] (int32, as lt_indexer_topk_paged writes them)."""
-    inputs, sizes, outputs, scratch = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse, workspace)
+    inputs, sizes, outputs, scratch, dev = _attention_args(dtype, q, pool, page_table, query_start, context_len, out, out_lse, workspace)
     T, topk = idx.shape
     if T != sizes[1]:
         raise ValueError("expected idx [T, topk]")
-    code = load().lt_kv4_attention_topk(*inputs, _dense(idx, _I32), topk, *sizes, scale, *outputs, *scratch,
+    code = load().lt_kv4_attention_topk(*inputs, _dense(idx, _I32, dev), topk, *sizes, scale, *outputs, *scratch,
                                         ctypes.byref(tunables) if tunables else None, _stream(stream))
     if code:
         _check(code, "lt_kv4_attention_topk")

@@ -803,7 +803,8 @@ int lt_dsa_union_mask(const int32_t* idx, int T, int topk, int N, int group, int
 // ---- serving step over the 4-bit cache ---------------------------------------------------------------------------------
 static bool kv4_shape(int Hkv, int D) { return Hkv > 0 && Hkv <= 1024 && (D == 64 || D == 128); }
 static bool kv4_dtype(int dtype) { return dtype == LT_DTYPE_BF16 || dtype == LT_DTYPE_F32; }
-// slots are int32
+// slots are int32, positions under 2^30
+constexpr int kKv4MostPages = 1 << 24, kKv4MostRequests = 1 << 20, kKv4MostTokens = 1 << 24;
 static bool kv4_pool(const void* pool, long long pages) {
   return pool != nullptr && aligned16(pool) && pages > 0 && pages <= INT_MAX / kPageKeys;
 }
@@ -817,7 +818,7 @@ int lt_page_tables(const int32_t* context_len, const int32_t* new_len, const int
                    int32_t* position, int32_t* status8, void* stream) {
   if (context_len == nullptr || new_len == nullptr || page_table == nullptr || total_len == nullptr || query_start == nullptr ||
       slot_map == nullptr || position == nullptr || status8 == nullptr || n_free < 0 || (n_free > 0 && free_pages == nullptr) ||
-      B <= 0 || B > (1 << 20) || max_pages <= 0 || max_pages > INT_MAX / kPageKeys || T <= 0 || total_len == context_len ||
+      B <= 0 || B > kKv4MostRequests || max_pages <= 0 || max_pages > kKv4MostPages || T <= 0 || T > kKv4MostTokens || total_len == context_len ||
       total_len == new_len)
     return LT_ERR_INVALID_ARG;
   LT_LAUNCH(launch_page_tables(context_len, new_len, free_pages, n_free, B, max_pages, T, page_table, total_len, query_start,
@@ -847,8 +848,12 @@ int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t
   return LT_OK;
 }
 
-// Rows of a request (or token) up to which the few-row kernel takes it, and from which the tiled kernel takes pairs of tiles.
-static constexpr int kKv4FewRows = 32, kKv4FewRowsTopk = 16, kKv4PairRows = 256;
+// Rows (tokens x heads of a group) of a request, or of a token with positions of its own, up to which the few-row kernel takes it, and from
+// which the tiled kernel takes pairs of tiles.  Measured in us, few-row / tile / pair, 4 key-value heads of 128, 32 requests over 4096 keys:
+// 32 rows 62 / 78 / 109, 48: 83 / 83 / 113, 64: 105 / 86 / 116, 128: 184 / 100 / 124, 192: 264 / 152 / 146, 512: 665 / 270 / 259 (2 requests over
+// 16,384: 48 rows 33 / 50 / 56, 128: 58 / 64 / 61, 256: 98 / 69 / 82); 512 tokens of 2 heads over 2048 positions each, few-row / tile:
+// 16 rows 128 / 240, 32: 229 / 246, 48: 328 / 255, 128: 823 / 302.
+static constexpr int kKv4FewRows = 48, kKv4FewRowsTopk = 32, kKv4PairRows = 192;
 
 static int kv4_attention_impl(int dtype, const void* q, long long q_stride, const void* pool, long long pool_pages,
                               const int32_t* page_table, int max_pages, const int32_t* query_start, const int32_t* context_len,
@@ -857,7 +862,7 @@ static int kv4_attention_impl(int dtype, const void* q, long long q_stride, cons
                               cudaStream_t stream) {
   if (!kv4_dtype(dtype) || (Hkv > 0 && !kv4_shape(Hkv, D))) return LT_ERR_UNSUPPORTED;
   if (q == nullptr || page_table == nullptr || query_start == nullptr || context_len == nullptr || out == nullptr || Hkv <= 0 ||
-      !kv4_pool(pool, pool_pages) || max_pages <= 0 || max_pages > INT_MAX / kPageKeys || B <= 0 || B > (1 << 20) || T <= 0 || Hq <= 0 || Hq % Hkv != 0 ||
+      !kv4_pool(pool, pool_pages) || max_pages <= 0 || max_pages > kKv4MostPages || B <= 0 || B > kKv4MostRequests || T <= 0 || T > kKv4MostTokens || Hq <= 0 || Hq % Hkv != 0 ||
       Hq > 65535 || static_cast<long long>(T) * Hq > INT_MAX || max_new < 0 || !isfinite(scale) || !aligned16(q) || !aligned16(out) ||
       q_stride < static_cast<long long>(Hq) * D || q_stride % (16 / static_cast<long long>(elem_bytes(dtype))) != 0)
     return LT_ERR_INVALID_ARG;

@@ -74,7 +74,8 @@ struct Kv4AttnParams {
   int min_rows, max_rows;    // requests with min_rows .. max_rows (token, head of the group) rows are this kernel's
 };
 
-// Tokens of request b: [first, first + n), clipped to the batch.
+// Tokens of request b: [first, first + n), clipped to the batch; ctx clipped to the table's reach, beyond which nothing is seen (so that
+// positions stay under 2^31: the reach and T are under 2^30 and 2^24).
 struct Kv4Request {
   int first, n, ctx;
 };
@@ -82,7 +83,8 @@ __device__ __forceinline__ Kv4Request kv4_request(const Kv4AttnParams& p, int b)
   int a = p.query_start[b], e = p.query_start[b + 1], c = p.context_len[b];
   a = a < 0 ? 0 : (a > p.T ? p.T : a);
   e = e < a ? a : (e > p.T ? p.T : e);
-  return {a, e - a, c < 0 ? 0 : c};
+  const int reach = p.max_pages * kPageKeys;
+  return {a, e - a, c < 0 ? 0 : (c < reach ? c : reach)};
 }
 
 }  // namespace lt

@@ -204,9 +204,22 @@ def test_large_and_tiny_queries():
 
 
 def test_fewer_ctas_give_results_within_the_same_bounds():
-    s = Step([700, 90, 3000], [1, 2, 1], 16, 2, 128, seed=8)
-    for grid in (1, 3, 50):
-        s.check(*s.run(grid=grid))
+    for new in ([1, 2, 1], [30, 2, 70]):
+        s = Step([700, 90, 3000], new, 16, 2, 128, seed=8)
+        for grid in (1, 3, 50):
+            s.check(*s.run(grid=grid), on_gpu_too=True)
+
+
+def test_lengths_beyond_the_table():
+    """A context longer than the table reaches, up to the largest number: the tokens see what the table holds."""
+    for ctx in (700, 1 << 30, 2**31 - 1):
+        for new in (1, 60):
+            s = Step([400], [new], 8, 2, 64, seed=11, poison=False)
+            s.table = np.ascontiguousarray(s.table[:, :5])
+            s.ctx[0] = ctx
+            out, lse = s.run()
+            s.ctx[0] = 319 + 60  # all tokens beyond the table's 320 positions
+            s.check(out, lse)
 
 
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right():

@@ -30,7 +30,7 @@ TABLES = dict(context_len=FAKE, new_len=FAKE, free_pages=FAKE, n_free=4, B=2, ma
 
 
 @pytest.mark.parametrize("change", [dict(context_len=NULL), dict(new_len=NULL), dict(free_pages=NULL), dict(n_free=-1), dict(B=0),
-                                    dict(B=(1 << 20) + 1), dict(max_pages=0), dict(max_pages=1 << 26), dict(T=0), dict(page_table=NULL), dict(total_len=NULL),
+                                    dict(B=(1 << 20) + 1), dict(max_pages=0), dict(max_pages=(1 << 24) + 1), dict(T=0), dict(T=(1 << 24) + 1), dict(page_table=NULL), dict(total_len=NULL),
                                     dict(total_len=FAKE), dict(query_start=NULL), dict(slot_map=NULL), dict(position=NULL),
                                     dict(status=NULL)], ids=str)
 def test_page_tables_refuses(lib, change):
@@ -66,7 +66,8 @@ REFUSED = [
     (dict(dtype=E4M3), UNSUPPORTED), (dict(D=192), UNSUPPORTED), (dict(q=NULL), INVALID), (dict(q=ODD), INVALID), (dict(q_stride=2040), INVALID),
     (dict(q_stride=2052), INVALID), (dict(pool=NULL), INVALID), (dict(pages=0), INVALID), (dict(page_table=NULL), INVALID),
     (dict(max_pages=0), INVALID), (dict(query_start=NULL), INVALID), (dict(context_len=NULL), INVALID), (dict(B=0), INVALID),
-    (dict(T=0), INVALID), (dict(Hq=12), INVALID), (dict(Hq=0), INVALID), (dict(Hkv=0), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(T=0), INVALID), (dict(T=(1 << 24) + 1), INVALID), (dict(B=(1 << 20) + 1), INVALID), (dict(max_pages=(1 << 24) + 1), INVALID),
+    (dict(T=1 << 20, Hq=1 << 15, q_stride=1 << 22), INVALID), (dict(Hq=12), INVALID), (dict(Hq=0), INVALID), (dict(Hkv=0), INVALID), (dict(scale=float("nan")), INVALID),
     (dict(scale=float("inf")), INVALID), (dict(out=NULL), INVALID), (dict(out=ODD), INVALID), (dict(workspace=NULL), WORKSPACE),
     (dict(workspace=0x1010), WORKSPACE), (dict(bytes=16), WORKSPACE),
     (dict(tunables=binding.Tunables(path=binding.LT_PATH_FUSED_ABS)), INVALID), (dict(tunables=binding.Tunables(path=9)), INVALID),
