@@ -10,8 +10,8 @@ namespace {
 // Two prefix sums over the requests say where each one's tokens and fresh pages begin; the tokens and pages are then dealt out
 // evenly over the CTAs, whichever requests they belong to.  Every CTA takes the sums itself (64 requests are one load per thread),
 // so that one launch does it all and no CTA waits for another; a fresh page's number is read from the free list, by its rank, where
-// it is needed.  Launch latency bounds it:
-// 8 us a call through the binding, 64 requests with one token each as well as 701 with 359 K.
+// it is needed.  Launch latency bounds it: 4 us of GPU time for 64 requests with one token each, 8 for 701 with 359 K tokens; a call
+// through the binding takes 7 either way.
 // ---------------------------------------------------------------------------------------------
 constexpr int kTabThreads = 1024;
 
@@ -161,8 +161,8 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const TablePar
 // Writer.  A thread takes 8 consecutive elements (one or two 16-byte loads), four threads share a group: two shuffles give its largest
 // magnitude.  16 threads (D = 128) hold a head's keys and the 16 beside them its values, so a warp writes whole rows.  It reads
 // 2 Hkv D elements a token and writes 9 / 16 byte for each; with 16 instructions an element it was bound by those, not by HBM
-// (65,536 tokens of 8 heads: 200 us), so ordinary groups of bf16 take a shorter way of 6: the quotient by a reciprocal and one
-// correction, the nibble from the bits of a sum that rounds.
+// (65,536 tokens of 8 heads of 128: 200 us), so ordinary groups of bf16 take a shorter way of 6: the quotient by a reciprocal and one
+// correction, the nibble from the bits of a sum that rounds: 98 us, 3.5 TB/s, 0.74 of the issue slots.
 // ---------------------------------------------------------------------------------------------
 constexpr int kCacheThreads = 256;
 constexpr int kCacheAhead = 4;  // loads in flight per thread
@@ -310,6 +310,7 @@ __global__ void __launch_bounds__(kCacheThreads) append_kernel(const AppendParam
 // ---------------------------------------------------------------------------------------------
 // Reader: the values that the cache holds, in the caller's type (rounded once); zeros where there is no slot.  A code with a constant
 // or-ed into an exponent is 128 + u (bf16 pairs: one more subtraction and the product, exact up to its rounding) or 2^23 + u (fp32).
+// 65,536 slots of 8 heads of 128 to bf16: 70 us, 4.9 TB/s.
 // ---------------------------------------------------------------------------------------------
 struct ReadParams {
   const uint8_t* pool;
