@@ -907,7 +907,7 @@ static int kv4_attention_impl(int dtype, const void* q, long long q_stride, cons
   const int few = idx != nullptr ? kKv4FewRowsTopk : kKv4FewRows;
   bool launched = false;
   if (idx == nullptr || most_rows <= few) {
-    p.max_rows = few;
+    if (most_rows > few) p.max_rows = few;  // (else there is no other kernel: it takes all requests, also where max_new says too little)
     LT_LAUNCH(launch_kv4_attention_rows(D, most_rows < few ? most_rows : few, p, scratch, p.ctl, grid, stream));
     ++g_launches;  // (two kernels)
     launched = true;
