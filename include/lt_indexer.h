@@ -349,10 +349,10 @@ int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t
  *   dtype         LT_DTYPE_BF16 (tensor cores) or LT_DTYPE_F32 (LT_PATH_GENERIC: fp32 arithmetic); type of q and out
  *   q             device: token t's Hq heads of D elements are dense at q + t * q_stride (elements); pointer and rows 16-byte
  *                 aligned.  Hq a multiple of Hkv, T * Hq < 2^31
- *   out, lse      device, [T][Hq][D] and [T][Hq] fp32 (or NULL), out 16-byte aligned
+ *   out, lse      device, [T][Hq][D] and [T][Hq] fp32 (or NULL), out 16-byte aligned; not in the memory of any input
  *   max_new       most tokens that any request adds in this step, or 0 if unknown.  It only decides which kernels are
  *                 launched: any value is safe, a right one is fastest
- *   scale         any finite number
+ *   scale         any finite number; scores (scale * q . k) have to stay under 10^8 in magnitude
  *   workspace     device, 256-byte aligned, at least lt_kv4_attention_workspace_bytes(...) bytes, scratch; one per stream
  *   tunables      path (AUTO, FUSED, GENERIC), grid (SMs to use) and wait_limit_us are used; NULL = defaults
  * q, and the keys and values of positions that some token sees, must be finite; what lies anywhere else in the pool is not

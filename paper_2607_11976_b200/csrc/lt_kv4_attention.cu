@@ -384,8 +384,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         off[nt][gi][0] = off[nt][gi][2] = __shfl_sync(0xffffffffu, sum, 8 * t);
         off[nt][gi][1] = off[nt][gi][3] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
       }
-      // (scores beyond 2^100 only have to stay finite: one key then has all the weight)
-      const float w = fminf(down * 16777216.f, 0x1p100f);
+      // (before it scores are under 2^13: at most 32 products under 2^-5 and a scale under 2^11 for each of 4 groups)
+      const float w = fminf(fmaxf(down * 16777216.f, kLeastWorth), 0x1p113f);
       worth[nt][0] = __shfl_sync(0xffffffffu, w, 8 * t);
       worth[nt][1] = __shfl_sync(0xffffffffu, w, 8 * t + 4);
     }
@@ -487,8 +487,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
             if (x > bar[nt][c]) {  // (the same in all lanes of the column)
-              const float now = kPShift - x * worth[nt][c], back = ex2(now - shift[nt][c]);
-              bar[nt][c] = x + kPSlack / worth[nt][c];
+              const float now = shift_of(x, worth[nt][c]), back = ex2(now - shift[nt][c]);
+              bar[nt][c] = bar_of(x, worth[nt][c]);
               shift[nt][c] = now;
               l[nt][c] *= back;
 #pragma unroll

@@ -13,7 +13,14 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // it multiplies all sums, and for 8 heads some score passes the exact maximum in every third unit): at most 2^15, and no less
 // than 2^-35 of the largest in fp16.
 constexpr float kPShift = 11.f, kPSlack = 4.f;
-constexpr float kNothing = 1e30f;  // shift of a row that has seen nothing
+constexpr float kNothing = 2e38f;  // shift of a row that has seen nothing: beyond all others, which are under 2^126
+// What a row's scores are worth in powers of two (query scaling, scale, log2 e), within bounds that keep products with the scores finite
+// and masked ones at -inf.  At the lower bound all scores are under 2^-60, which no weight shows.
+constexpr float kLeastWorth = 0x1p-100f;
+// What is added to a score top * worth for it to become kPShift, and the score up to which that stays: rounded down, so that no
+// probability passes 2^15 however coarse fp32 is at that size.  (At 2^28 the largest then comes out as 2^-5 to 2^11.)
+__device__ __forceinline__ float shift_of(float top, float worth) { return __fmaf_rd(-top, worth, kPShift); }
+__device__ __forceinline__ float bar_of(float top, float worth) { return __fadd_rd(top, kPSlack / worth); }
 
 // ---- arithmetic -------------------------------------------------------------------------------
 __device__ __forceinline__ float ex2(float x) {

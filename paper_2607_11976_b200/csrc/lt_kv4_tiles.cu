@@ -540,7 +540,8 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
         }
         const int e = max(static_cast<int>(top >> 7), 21);
         const float up = copysignf(__uint_as_float(static_cast<uint32_t>(127 + 127 + 15 - e) << 23), p.scale);
-        worth = fminf(__uint_as_float(static_cast<uint32_t>(e - 15) << 23) * to_log2, 0x1p80f);
+        // (before it scores are under 2^37: 128 products of 2^16 and 2^14 at most)
+        worth = fminf(fmaxf(__uint_as_float(static_cast<uint32_t>(e - 15) << 23) * to_log2, kLeastWorth), 0x1p89f);
 #pragma unroll 4
         for (int i = 0; i < D / 8; ++i) {
           uint4 x = make_uint4(0, 0, 0, 0);
@@ -643,9 +644,9 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
         if (__builtin_expect(__any_sync(0xffffffffu, grows), 0)) {
           float back = 1.f;
           if (grows) {
-            const float now = kPShift - top * worth;
+            const float now = shift_of(top, worth);
             back = ex2(now - shift);
-            worth_bar = top + kPSlack / worth;
+            worth_bar = bar_of(top, worth);
             shift = now;
             l *= back;
           }

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 import kv4_util as ku
+from oracle import kv4
 from paper_2607_11976_b200 import binding as lt
 
 pytestmark = pytest.mark.gpu
@@ -17,3 +18,38 @@ def test_a_wrong_max_new_only_costs_time(max_new, D):
     s = ku.Step([100, 3, 700, 0], [1, 40, 100, 260], 16, 2, D, seed=1)
     out, lse = s.run(max_new=max_new)
     s.check(out, lse)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-30, 1e-12, -1e-12])
+@pytest.mark.parametrize("new", [[1, 2], [300, 70]], ids=str)
+@pytest.mark.parametrize("D", [64, 128])
+def test_zero_queries_and_tiny_scales_average_the_values(scale, new, D):
+    """All weights are equal then, whatever is masked beside them."""
+    s = ku.Step([70, 3], new, 8, 2, D, seed=2, pad=1)
+    s.scale = scale
+    s.q[::2] = 0
+    s.q[1::2, :3] = 2.0**-120
+    out, lse = s.run(max_new=max(new))
+    s.check(out, lse)
+    idx = s.selection(40, duplicates=True)
+    out, lse = s.run(idx=idx)
+    s.check(out, lse, idx)
+
+
+@pytest.mark.parametrize("gain", [1e3, 1e5, 1e6, 2.5e7])
+@pytest.mark.parametrize("new", [[1, 2], [300, 70]], ids=str)
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_far_below_zero(gain, new, D):
+    """Tokens that see one key, or few, whose scores are all far from zero: rounding them must not make a weight overflow or vanish.
+    (What a token that sees one key gets is that key's value, whatever the score, but for the roundings of weight, value and result.)"""
+    s = ku.Step([0, 3], new, 8, 2, D, seed=3, q_gain=gain)
+    out, lse = s.run(max_new=max(new))
+    s.check(out, lse)
+    row = s.pool[s.table[0, 0], :, 0]
+    value = kv4.unpack_rows(row)[1]
+    assert (np.abs(out[0] - value.repeat(4, 0)) <= (2.0**-8 + 2.0**-10) * np.abs(value).repeat(4, 0)).all()
+    idx = s.selection(2)
+    out, lse = s.run(idx=idx)
+    s.check(out, lse, idx)
+    value = value * (idx[0] == 0).any()  # (a row that names nothing it sees gets zeros)
+    assert (np.abs(out[0] - value.repeat(4, 0)) <= (2.0**-8 + 2.0**-10) * np.abs(value).repeat(4, 0)).all()
