@@ -293,8 +293,9 @@ int lt_dsa_union_mask(const int32_t* idx, int T, int topk, int N, int group,
  * so values beyond 14,336 saturate, and NaN is stored as 0.  D is 64 or 128.
  *
  * Requests.  B of them in consecutive rows of the step's batch: request b has rows query_start[b] .. query_start[b + 1] - 1
- * (ascending), and row query_start[b] + j stands at position context_len[b] + j.  Rows from query_start[B] on are padding:
- * no output is written there.  Positions 64 j .. 64 j + 63 of request b lie in page page_table[b][j].  A position whose table
+ * (ascending), and row query_start[b] + j stands at position context_len[b] + j.  Rows before query_start[0] and
+ * from query_start[B] on belong to no request: no output is written there (a part of the requests may be given, by pointers into
+ * query_start, context_len and page_table).  Positions 64 j .. 64 j + 63 of request b lie in page page_table[b][j].  A position whose table
  * entry is no page of the pool, or lies beyond the table, is seen by no token.  Limits: B <= 2^20, T <= 2^24, max_pages <= 2^24,
  * Hkv <= 1024, fewer than 2^31 rows in the pool.
  * ---------------------------------------------------------------------------------------------

@@ -86,5 +86,14 @@ __device__ __forceinline__ Kv4Request kv4_request(const Kv4AttnParams& p, int b)
   const int reach = p.max_pages * kPageKeys;
   return {a, e - a, c < 0 ? 0 : (c < reach ? c : reach)};
 }
+// Rows of the batch that belong to requests: [first, end).
+struct Kv4Rows {
+  int first, end;
+};
+__device__ __forceinline__ Kv4Rows kv4_rows(const Kv4AttnParams& p) {
+  int a = p.query_start[0], e = p.query_start[p.B];
+  a = a < 0 ? 0 : (a > p.T ? p.T : a);
+  return {a, e < a ? a : (e > p.T ? p.T : e)};
+}
 
 }  // namespace lt

@@ -160,15 +160,14 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
   };
   Cursor<D, NT, kTopk> at;
   if constexpr (kTopk) {
-    int end = p.query_start[p.B];
-    end = end < 0 ? 0 : (end > p.T ? p.T : end);
+    const Kv4Rows rows = kv4_rows(p);
     const int units = (p.topk + kUnit - 1) / kUnit, tiles = (p.group + S::kRows - 1) / S::kRows;
     const long long per = static_cast<long long>(units) * tiles * p.Hkv;
-    total = per * end;
+    total = per * (rows.end - rows.first);
     cut();
     if (lo < hi) {
       const long long token = quotient(lo, per);
-      at.start(p, static_cast<int>(token), lo - token * per);
+      at.start(p, rows.first + static_cast<int>(token), lo - token * per);
     }
   } else {
     RequestWork<D, NT> w;

@@ -11,9 +11,10 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162f
 __device__ __forceinline__ void store_out(float* at, float x) { *at = x; }
 __device__ __forceinline__ void store_out(__nv_bfloat16* at, float x) { *at = __float2bfloat16_rn(x); }
 
-// The request of a token: the last b with query_start[b] <= t that has tokens at t; -1 behind the last request.
+// The request of a token: the last b with query_start[b] <= t that has tokens at t; -1 outside of all.
 __device__ __forceinline__ int request_of(const Kv4AttnParams& p, int t) {
-  if (t >= p.query_start[p.B]) return -1;
+  const Kv4Rows rows = kv4_rows(p);
+  if (t < rows.first || t >= rows.end) return -1;
   int lo = 0, hi = p.B;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;

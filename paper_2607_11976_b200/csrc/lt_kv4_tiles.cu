@@ -393,18 +393,18 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
     };
     if constexpr (kTopk) {
       if (tid == 0) {
-        int end = p.query_start[p.B];
-        end = end < 0 ? 0 : (end > p.T ? p.T : end);
+        const Kv4Rows rows = kv4_rows(p);
         const int units = (p.topk + kKeys - 1) / kKeys, tiles = (p.group + C::kRows - 1) / C::kRows;
         const long long per = static_cast<long long>(units) * tiles * p.Hkv;
         long long lo, hi;
-        cut(per * end, lo, hi);
+        cut(per * (rows.end - rows.first), lo, hi);
         sh.lo = lo;
         sh.hi = hi;
         if (lo < hi) {
           long long off = lo;
-          sh.b = static_cast<int>(quotient(off, per));
-          off -= per * sh.b;
+          const long long token = quotient(off, per);
+          sh.b = rows.first + static_cast<int>(token);
+          off -= per * token;
           const long long item = quotient(off, units);
           sh.unit = static_cast<int>(off - item * units);
           sh.kvh = static_cast<int>(quotient(item, tiles));

@@ -53,3 +53,17 @@ def test_scores_far_below_zero(gain, new, D):
     s.check(out, lse, idx)
     value = value * (idx[0] == 0).any()  # (a row that names nothing it sees gets zeros)
     assert (np.abs(out[0] - value.repeat(4, 0)) <= (2.0**-8 + 2.0**-10) * np.abs(value).repeat(4, 0)).all()
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv", [("bf16", 8, 2), ("bf16", 80, 2), ("f32", 8, 2)])
+@pytest.mark.parametrize("selected", [False, True])
+def test_a_part_of_the_requests(selected, dtype, Hq, Hkv):
+    """Tables from the second request on: the first one's rows are left as they were."""
+    s = ku.Step([50, 90, 400], [30, 1, 70], Hq, Hkv, 64, dtype, seed=4, pad=2)
+    idx = s.selection(60) if selected else None
+    n = int(s.new[0])
+    s.start, s.ctx, s.new, s.table = s.start[1:], s.ctx[1:], s.new[1:], s.table[1:]
+    out, lse = s.run(idx=idx)
+    assert (out[:n] == 7.0).all() and (lse[:n] == 7.0).all()
+    s.start, s.q, s.T = s.start - n, s.q[n:], s.T - n
+    s.check(out[n:], lse[n:], None if idx is None else idx[n:], fused=dtype == "bf16")
