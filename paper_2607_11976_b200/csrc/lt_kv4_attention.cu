@@ -131,8 +131,15 @@ struct Cursor {
     if (++kvh < p.Hkv) return;
     kvh = 0;
     ++b;
-    if constexpr (!kTopk)
-      while (b < p.B && w.load(p, b) == 0) ++b;
+    if constexpr (!kTopk) {
+      if (b < p.B && w.load(p, b) == 0) {
+        b = next_request(p, b + 1, [&](const Kv4Request& r) {
+          const long long rows = static_cast<long long>(r.n) * p.group;
+          return rows >= p.min_rows && rows <= p.max_rows;
+        });
+        if (b < p.B) w.load(p, b);
+      }
+    }
   }
   __device__ __forceinline__ void next(const Kv4AttnParams& p, bool more) {
     if (++unit == w.units && more) next_item(p);
@@ -232,20 +239,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
     near_pos = near_page = -1;
     if (!any) return;
     if (token != req_token) {
-      // 32 requests at a look: the last one that begins at or before the token
-      if (req_token < 0) {
-        int a = 0, n = p.B;
-        while (n > 1) {
-          const int step = (n + 31) / 32, i = lane * step;
-          const unsigned le = __ballot_sync(0xffffffffu, i < n && p.query_start[a + i] <= token);
-          const int hit = (31 - __clz(le | 1u)) * step;
-          a += hit;
-          n = n - hit < step ? n - hit : step;
-        }
-        req_b = a;
-      } else {
-        while (req_b + 1 < p.B && p.query_start[req_b + 1] <= token) ++req_b;
-      }
+      req_b = req_token < 0 ? request_of_row(p, token) : request_of_row_from(p, req_b, token);
       req = kv4_request(p, req_b);
       req_token = token;
     }

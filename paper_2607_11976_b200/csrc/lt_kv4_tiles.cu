@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kTileRows = 128;
 constexpr int kStep = 32;       // rows of a stage of the ring
-constexpr int kKnown = 128;
+constexpr int kKnown = 1024;    // requests whose work is kept from the first look to the second
 constexpr int kSeenStages = 4;  // tiles whose visible keys are noted at once
 
 template <int D, int kTiles>
@@ -54,8 +54,6 @@ struct Shared {
   unsigned there[kSeenStages][4];  // a bit per key of the tile
   int abort_flag[2], drain_flag[2];  // [1]: limit of a wait in microseconds (lt_ptx.cuh)
   uint32_t tmem;
-  long long units[kKnown];  // of one head of the first requests
-  int tiles[kKnown];
   long long sums[16];
   // where the CTA's run begins
   long long lo, hi;
@@ -83,6 +81,44 @@ __device__ __forceinline__ long long request_units(const Kv4AttnParams& p, const
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   return sum;
+}
+
+// Units of one head of request b (zero where there is none) and its tiles, for the requests of a warp's lanes.
+template <int kRows, int kKeys>
+__device__ __forceinline__ long long units_of_lanes(const Kv4AttnParams& p, int b, int& tiles) {
+  constexpr int kFew = 4;  // tiles that a lane goes through by itself
+  Kv4Request r{0, 0, 0};
+  tiles = 0;
+  if (b < p.B) {
+    r = kv4_request(p, b);
+    tiles = request_tiles<kRows>(p, r);
+  }
+  long long per = 0;
+  if (tiles <= kFew)
+    for (int rt = 0; rt < tiles; ++rt) per += item_units<kRows, kKeys>(p, r, rt);
+  for (unsigned many = __ballot_sync(0xffffffffu, tiles > kFew); many != 0; many &= many - 1) {
+    const int j = __ffs(many) - 1;
+    const Kv4Request x{__shfl_sync(0xffffffffu, r.first, j), __shfl_sync(0xffffffffu, r.n, j), __shfl_sync(0xffffffffu, r.ctx, j)};
+    const long long sum = request_units<kRows, kKeys>(p, x, __shfl_sync(0xffffffffu, tiles, j));
+    if ((threadIdx.x & 31) == j) per = sum;
+  }
+  return per;
+}
+
+// The first request from b on that has tiles; out of line, so that the roles' loops stay together (2048 tokens over 30 K: 1430 us with
+// it in each role, 1340).
+__device__ __noinline__ int next_tiled_request(const int32_t* query_start, const int32_t* context_len, int B, int T, int group, int min_rows,
+                                               int max_rows, int b) {
+  Kv4AttnParams p{};
+  p.query_start = query_start;
+  p.context_len = context_len;
+  p.max_pages = 1;  // (lengths do not matter here)
+  p.B = B;
+  p.T = T;
+  p.group = group;
+  p.min_rows = min_rows;
+  p.max_rows = max_rows;
+  return next_request(p, b, [&](const Kv4Request& x) { return request_tiles<kTileRows>(p, x) > 0; });
 }
 
 // Where a role stands: every role walks through the CTA's run by itself.
@@ -127,14 +163,15 @@ struct Walk {
       return true;
     }
     kvh = 0;
-    do {
-      ++b;
-      if (!kTopk && b >= p.B) {
+    ++b;
+    if constexpr (!kTopk) {
+      b = next_tiled_request(p.query_start, p.context_len, p.B, p.T, p.group, p.min_rows, p.max_rows, b);
+      if (b >= p.B) {
         left = 0;
         return false;
       }
-      request(p);
-    } while (!kTopk && units == 0);
+    }
+    request(p);
     return true;
   }
 };
@@ -415,18 +452,22 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
       // An item costs its units and, for its queries and results, as much as kItemCost more: runs are cut evenly in that measure.  (By units
       // alone a run of short items, a prompt's first chunk, took 1.7 times the average: a mixed batch 256 us instead of 176.)
       constexpr int kItemCost = 256 / kKeys;
-      // the total: a request per warp and turn; what a head of the first ones takes is kept
+      // the total: 32 requests per warp and turn; what a head of the first ones takes is kept, where the first keys will come
+      static_assert(kKnown * 12 <= C::kStages * C::kTileBytes, "room for the known requests");
+      long long* known_units = reinterpret_cast<long long*>(smem_raw + (s_k - ptx::smem_u32(smem_raw)));
+      int* known_tiles = reinterpret_cast<int*>(known_units + kKnown);
       long long sum = 0;
-      for (int b = warp; b < p.B; b += C::kWarps) {
-        const Kv4Request r = kv4_request(p, b);
-        const int tiles = request_tiles<C::kRows>(p, r);
-        const long long per = tiles > 0 ? request_units<C::kRows, kKeys>(p, r, tiles) : 0;
-        if (lane == 0 && b < kKnown) {
-          sh.units[b] = per;
-          sh.tiles[b] = tiles;
+      for (int b0 = warp * 32; b0 < p.B; b0 += C::kWarps * 32) {
+        int tiles;
+        const long long per = units_of_lanes<C::kRows, kKeys>(p, b0 + lane, tiles);
+        if (b0 + lane < kKnown) {
+          known_units[b0 + lane] = per;
+          known_tiles[b0 + lane] = tiles;
         }
         sum += (per + tiles * kItemCost) * p.Hkv;
       }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
       if (lane == 0) sh.sums[warp] = sum;
       __syncthreads();
       if (warp < 2) {  // where the run begins, and where the next one does
@@ -435,20 +476,38 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
         cut(total, lo, hi);
         const long long x = warp == 0 ? lo : hi;
         long long before = 0, units_before = 0, per = 0;
-        int b = 0, tiles = 0;
-        for (; b < p.B; ++b) {
-          if (b < kKnown) {
-            per = sh.units[b];
-            tiles = sh.tiles[b];
+        int b = p.B, tiles = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+          int my_tiles;
+          long long mine;
+          if (b0 + 32 <= kKnown) {
+            mine = known_units[b0 + lane];
+            my_tiles = known_tiles[b0 + lane];
           } else {
-            const Kv4Request r = kv4_request(p, b);
-            tiles = request_tiles<C::kRows>(p, r);
-            per = tiles > 0 ? request_units<C::kRows, kKeys>(p, r, tiles) : 0;
+            mine = units_of_lanes<C::kRows, kKeys>(p, b0 + lane, my_tiles);
           }
-          const long long cost = (per + tiles * kItemCost) * p.Hkv;
-          if (x < before + cost) break;
-          before += cost;
-          units_before += per * p.Hkv;
+          const long long cost = (mine + my_tiles * kItemCost) * p.Hkv;
+          long long costs = cost, units = mine * p.Hkv;  // up to and with this lane's
+#pragma unroll 1
+          for (int d = 1; d < 32; d <<= 1) {
+            const long long c = __shfl_up_sync(0xffffffffu, costs, d), u = __shfl_up_sync(0xffffffffu, units, d);
+            if (lane >= d) {
+              costs += c;
+              units += u;
+            }
+          }
+          const unsigned beyond = __ballot_sync(0xffffffffu, x < before + costs);
+          const int j = beyond != 0 ? __ffs(beyond) - 1 : 31;
+          if (beyond != 0) {
+            b = b0 + j;
+            per = __shfl_sync(0xffffffffu, mine, j);
+            tiles = __shfl_sync(0xffffffffu, my_tiles, j);
+            before += __shfl_sync(0xffffffffu, costs - cost, j);
+            units_before += __shfl_sync(0xffffffffu, units - mine * p.Hkv, j);
+            break;
+          }
+          before += __shfl_sync(0xffffffffu, costs, j);
+          units_before += __shfl_sync(0xffffffffu, units, j);
         }
         int kvh = 0, my_rt = 0, my_unit = 0;
         bool here = b == p.B && lane == 0;  // (the end of all runs)
@@ -849,15 +908,14 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
     // ---- rows: a lane has a key of each step; the next tile's positions and pages are looked up while this one's are copied -----------
     Turn<C::kRing> ring;
     Turn<kSeenStages> seen;
-    int req_b = 0;
+    int req_b = -1;
     long long last = 0;  // the last position that any row of the item sees
     const int32_t* table = p.page_table;
     auto item = [&]() {
       Kv4Request r = at.r;
       int b = at.b;
       if constexpr (kTopk) {
-        while (req_b + 1 < p.B && p.query_start[req_b + 1] <= at.b) ++req_b;
-        b = req_b;
+        b = req_b = req_b < 0 ? request_of_row(p, at.b) : request_of_row_from(p, req_b, at.b);
         r = kv4_request(p, b);
         last = static_cast<long long>(r.ctx) + (at.b - r.first);
       } else {

@@ -67,3 +67,31 @@ def test_a_part_of_the_requests(selected, dtype, Hq, Hkv):
     assert (out[:n] == 7.0).all() and (lse[:n] == 7.0).all()
     s.start, s.q, s.T = s.start - n, s.q[n:], s.T - n
     s.check(out[n:], lse[n:], None if idx is None else idx[n:], fused=dtype == "bf16")
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 64), (4, 1, 128)])
+@pytest.mark.parametrize("kind", ["slots", "decode", "chunks"])
+def test_many_requests(kind, Hq, Hkv, D):
+    """Slots that are mostly empty, decoding requests with a few prompts between them, and short chunks: more requests than a CTA
+    keeps in mind."""
+    rng = np.random.default_rng(5)
+    B = 1500
+    new = {"slots": np.zeros(B, int), "decode": np.ones(B, int), "chunks": rng.integers(0, 18, B)}[kind]
+    if kind != "chunks":
+        new[[0, 40, 77, 1029, 1400, B - 1]] = [70, 1, 150, 40, 300, 2]
+    ctx = np.where(new > 0, rng.integers(0, 90, B), 0)
+    s = ku.Step(ctx, new, Hq, Hkv, D, seed=6)
+    out, lse = s.run(max_new=int(new.max()))
+    s.check(out, lse, on_gpu_too=True)
+
+
+@pytest.mark.parametrize("Hq", [8, 40])
+def test_many_requests_with_positions_of_their_own(Hq):
+    rng = np.random.default_rng(7)
+    new = np.zeros(1500, int)
+    new[rng.integers(0, 1500, 90)] = 1
+    new[[0, 700]] = [0, 9]
+    s = ku.Step(np.where(new > 0, rng.integers(0, 200, 1500), 0), new, Hq, 1, 64, seed=8)
+    idx = s.selection(70)
+    out, lse = s.run(idx=idx)
+    s.check(out, lse, idx, on_gpu_too=True)
