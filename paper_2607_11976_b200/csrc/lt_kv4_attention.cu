@@ -24,8 +24,8 @@
 // sees whole it writes out itself; the parts of others are joined first within the CTA, then, where an item spans CTAs, by a
 // second kernel.  Runs are a matter of the lengths alone, so results do not vary.
 //
-// Measured: 64 requests of up to 32 K positions, 8 key-value heads of 128 with 8 query heads each: 1.21 GB in 270 us, 4.5 TB/s, 0.68 of
-// the copy rate (one request of 1 M: 260 us, 0.71).  Instructions bound it: 298 for 16 keys of a head (by count 40 masks and shifts for the
+// Measured: 64 requests of up to 32 K positions, 8 key-value heads of 128 with 8 query heads each: 1.21 GB in 279 us, 4.3 TB/s, 0.66 of
+// the copy rate (one request of 1 M: 269 us, 0.68).  Instructions bound it: 300 for 16 keys of a head (by count 40 masks and shifts for the
 // keys, 48 and 58 of fp16 arithmetic for the values), 0.64 of the issue slots with 3 warps to a scheduler; at 335 it took, without its
 // loads, still 0.91 of its time.
 #include "lt_kv4_parts.cuh"

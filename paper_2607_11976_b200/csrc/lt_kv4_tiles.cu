@@ -12,9 +12,9 @@
 // (8192 bf16 flops a clock) and 1024 of exponentials (16 a clock): the two bound this together.  The roles' loops are kept short on purpose:
 // with everything unrolled the warps of an SM waited for instructions most of the time (a chunk of 2048 over 30 K: 2.5 ms, loops 1.8).
 //
-// Measured: that chunk (32 query heads on 4 key-value heads of 128) 1.33 ms, 805 TFLOP/s, 0.50 of the measured bf16 burst: tensor cores at
+// Measured: that chunk (32 query heads on 4 key-value heads of 128) 1.35 ms, 795 TFLOP/s, 0.49 of the measured bf16 burst: tensor cores at
 // work 0.38 of the clocks, exponentials 0.38, issue slots 0.45; what is left is each tile's chain, 3.3 thousand clocks of softmax and 2.1 until
-// its next scores.  1024 tokens of 64 heads over 2048 positions of one key-value head 262 us, bound by unpacking and by the same chain.
+// its next scores.  1024 tokens of 64 heads over 2048 positions of one key-value head 268 us, bound by unpacking and by the same chain.
 //
 // Column c = 8 m + i of a key tile is key 8 m + (m + i) % 8: then 8 neighbouring rows of the ring, and the 8 columns of a 16-byte
 // piece of the transposed values, are read and written in different banks.  Elements are paired as the codes come, (i, i + 4) of every
