@@ -316,8 +316,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
 #pragma unroll
   for (int i = 0; i < S::kStages - 1; ++i) fetch();
 
-  // (a scale of zero is taken as a tiny one, so that what is masked stays at -inf; a negative one turns the queries' signs)
-  const float to_log2 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);
   // ---- the run ----------------------------------------------------------------------------------
   if (lane < 2) s_part[warp][lane] = PartDesc{0, 0, 0, 0};
   int stage = 0;
@@ -355,8 +353,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int e = max(static_cast<int>(top >> 7), 21);  // biased exponent; rows under 2^-106 stay smaller
+      // (a negative scale turns the queries' signs)
       const float up = copysignf(__uint_as_float(static_cast<uint32_t>(127 + 127 + 15 - e) << 23), p.scale);
-      const float down = __uint_as_float(static_cast<uint32_t>(e - 15) << 23) * to_log2;
 #pragma unroll
       for (int gi = 0; gi < S::kGroups; ++gi) {
         const uint32_t w[4] = {x[gi].x, x[gi].y, x[gi].z, x[gi].w};
@@ -378,7 +376,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_rows_kern
         off[nt][gi][1] = off[nt][gi][3] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
       }
       // (before it scores are under 2^13: at most 32 products under 2^-5 and a scale under 2^11 for each of 4 groups)
-      const float w = fminf(fmaxf(down * 16777216.f, kLeastWorth), 0x1p113f);
+      const float w = worth_of(e, p.scale, 16777216.f, 0x1p113f);
       worth[nt][0] = __shfl_sync(0xffffffffu, w, 8 * t);
       worth[nt][1] = __shfl_sync(0xffffffffu, w, 8 * t + 4);
     }

@@ -17,6 +17,13 @@ constexpr float kNothing = 2e38f;  // shift of a row that has seen nothing: beyo
 // What a row's scores are worth in powers of two (query scaling, scale, log2 e), within bounds that keep products with the scores finite
 // and masked ones at -inf.  At the lower bound all scores are under 2^-60, which no weight shows.
 constexpr float kLeastWorth = 0x1p-100f;
+// That worth for a row whose queries were multiplied by 2^(142 - e): 2^(e - 142) |scale| log2(e) gain, gain a power of two from 1 to 2^24.
+// The first product can leave fp32's range: where it falls below, the result is under kLeastWorth (a scale of zero too), where it passes
+// it, beyond `most`.
+__device__ __forceinline__ float worth_of(int e, float scale, float gain, float most) {
+  const float down = __uint_as_float(static_cast<uint32_t>(e - 15) << 23) * fabsf(scale);
+  return fminf(fmaxf(down * (gain * kLog2e), kLeastWorth), most);
+}
 // What is added to a score top * worth for it to become kPShift, and the score up to which that stays: rounded down, so that no
 // probability passes 2^15 however coarse fp32 is at that size.  (At 2^28 the largest then comes out as 2^-5 to 2^11.)
 __device__ __forceinline__ float shift_of(float top, float worth) { return __fmaf_rd(-top, worth, kPShift); }

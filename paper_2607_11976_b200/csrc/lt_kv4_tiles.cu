@@ -568,7 +568,6 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
     const int tt = warp >> 2, r128 = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + tt * 128, t_o = tmem + lanes + kTiles * 128 + tt * 128;
-    const float to_log2 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);
     Turn<kSeenStages> seen;
     uint32_t s_phase[2] = {0, 0}, o_uses[2] = {0, 0};  // (o_uses: parity of the products that were asked for from a buffer)
     int buf = 0;
@@ -600,7 +599,7 @@ attention_tiles_kernel(const Kv4AttnParams p, const SplitBuffers sb) {
         const int e = max(static_cast<int>(top >> 7), 21);
         const float up = copysignf(__uint_as_float(static_cast<uint32_t>(127 + 127 + 15 - e) << 23), p.scale);
         // (before it scores are under 2^37: 128 products of 2^16 and 2^14 at most)
-        worth = fminf(fmaxf(__uint_as_float(static_cast<uint32_t>(e - 15) << 23) * to_log2, kLeastWorth), 0x1p89f);
+        worth = worth_of(e, p.scale, 1.f, 0x1p89f);
 #pragma unroll 4
         for (int i = 0; i < D / 8; ++i) {
           uint4 x = make_uint4(0, 0, 0, 0);
