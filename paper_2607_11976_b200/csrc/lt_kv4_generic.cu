@@ -1,4 +1,6 @@
 // Attention over the 4-bit cache in fp32 throughout: the path of fp32 queries, and the plain reading of the method.
+#include <float.h>
+
 #include "lt_kv4.cuh"
 
 namespace lt {
@@ -54,7 +56,10 @@ __global__ void __launch_bounds__(kGenWarps * 32) attention_generic_kernel(const
   if (b < 0) return;
   const Kv4Request r = kv4_request(p, b);
   const In* q = static_cast<const In*>(p.q) + t * p.q_stride + (static_cast<long long>(kvh) * p.group + h0) * D;
-  for (int i = tid; i < kHeads * D; i += kGenWarps * 32) s_q[i / D][i % D] = i / D < n_heads ? to_float(q[i]) * p.scale : 0.f;
+  for (int i = tid; i < kHeads * D; i += kGenWarps * 32) {
+    const float x = i / D < n_heads ? to_float(q[i]) * p.scale : 0.f;
+    s_q[i / D][i % D] = isinf(x) ? copysignf(FLT_MAX, x) : x;  // (so that a key element of zero leaves zero)
+  }
   __syncthreads();
   const long long last = static_cast<long long>(r.ctx) + (t - r.first);  // the token's own position
   const long long reach = static_cast<long long>(p.max_pages) * kPageKeys;

@@ -27,3 +27,15 @@ def test_scales_and_queries_at_the_ends_of_their_range(dtype, path, scale, gain,
     s = ku.Step([300, 40], new, Hq, 1, D, dtype, seed=3, pad=1, q_gain=gain)
     s.scale = float(np.float32(scale))
     _both_forms(s, path, dtype == "bf16" and path != lt.LT_PATH_GENERIC)
+
+
+@pytest.mark.parametrize("dtype,path", PATHS, ids=IDS)
+@pytest.mark.parametrize("new,Hq", [([1, 2], 8), ([30, 70], 64)], ids=str)
+@pytest.mark.parametrize("scale", [1e37, -3.4e38])
+def test_keys_of_zero_under_a_large_scale(dtype, path, new, Hq, scale):
+    """All scores are zero, although scale * q is beyond fp32."""
+    s = ku.Step([300, 40], new, Hq, 1, 64, dtype, seed=5, q_gain=100.0, poison=False)
+    for rows in (s.pool, s.clean):
+        rows[..., :32], rows[..., 64:68] = 0x88, 0  # key codes and key scales
+    s.scale = float(np.float32(scale))
+    _both_forms(s, path, dtype == "bf16" and path != lt.LT_PATH_GENERIC)
