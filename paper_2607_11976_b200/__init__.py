@@ -13,6 +13,7 @@ from .binding import (  # noqa: F401
     LT_PATH_GENERIC,
     LtError,
     Tunables,
+    alloc_kv4_pool,
     lt_indexer_scores,
     lt_indexer_topk,
     lt_indexer_topk_ex,
@@ -22,6 +23,7 @@ from .binding import (  # noqa: F401
     lt_kv4_attention,
     lt_kv4_attention_topk,
     lt_kv4_attention_workspace_bytes,
+    lt_kv4_page_bytes,
     lt_kv4_read,
     lt_page_tables,
     lt_read_status,
