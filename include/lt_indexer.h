@@ -316,7 +316,8 @@ size_t lt_kv4_page_bytes(int Hkv, int D); /* 0 for a D or Hkv that is not suppor
  *   status8       device, 8 int32: [0] LT_STATUS_SHORT if free pages ran out, a request needs more than max_pages pages, the
  *                 tokens are more than T, or a length is negative (it counts as 0); [1] tokens of the step, [2] pages handed
  *                 out (the caller's free list then starts that much later), [3] pages that were missing; the rest 0
- * Pages that are missing are entered as -1.  total_len must not be context_len or new_len.  Integer work only: exact.
+ * Pages that are missing are entered as -1.  total_len must not overlap context_len or new_len (refused), and no other output may
+ * overlap an input or another output.  Integer work only: exact.
  */
 int lt_page_tables(const int32_t* context_len, const int32_t* new_len, const int32_t* free_pages, int n_free, int B,
                    int max_pages, int T, int32_t* page_table, int32_t* total_len, int32_t* query_start, int32_t* slot_map,

@@ -818,9 +818,14 @@ int lt_page_tables(const int32_t* context_len, const int32_t* new_len, const int
                    int32_t* position, int32_t* status8, void* stream) {
   if (context_len == nullptr || new_len == nullptr || page_table == nullptr || total_len == nullptr || query_start == nullptr ||
       slot_map == nullptr || position == nullptr || status8 == nullptr || n_free < 0 || (n_free > 0 && free_pages == nullptr) ||
-      B <= 0 || B > kKv4MostRequests || max_pages <= 0 || max_pages > kKv4MostPages || T <= 0 || T > kKv4MostTokens || total_len == context_len ||
-      total_len == new_len)
+      B <= 0 || B > kKv4MostRequests || max_pages <= 0 || max_pages > kKv4MostPages || T <= 0 || T > kKv4MostTokens)
     return LT_ERR_INVALID_ARG;
+  // (one CTA writes the new lengths while others still read the old ones)
+  auto meet = [&](const int32_t* a, const int32_t* b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return (x < y ? y - x : x - y) < static_cast<uintptr_t>(B) * sizeof(int32_t);
+  };
+  if (meet(total_len, context_len) || meet(total_len, new_len)) return LT_ERR_INVALID_ARG;
   LT_LAUNCH(launch_page_tables(context_len, new_len, free_pages, n_free, B, max_pages, T, page_table, total_len, query_start,
                                slot_map, position, status8, static_cast<cudaStream_t>(stream)));
   return LT_OK;
