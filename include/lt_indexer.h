@@ -281,7 +281,9 @@ int lt_dsa_union_mask(const int32_t* idx, int T, int topk, int N, int group,
  *     lt_indexer_topk_paged     (sparse attention) the positions each token reads; row b of page_table is request b's table
  *     lt_kv4_attention          causal attention over all positions, or
  *     lt_kv4_attention_topk     over the selected ones
- * All lengths live on the device: the calls of a step can be captured into one CUDA graph and replayed as the requests grow.
+ * The lengths that lt_page_tables, lt_kv4_append and both forms of attention go by live on the device: captured into a CUDA graph, these
+ * calls follow them at every replay.  lt_indexer_topk_paged takes a request's N, topk and causal_offset from the host: a captured
+ * call would go on selecting from the lengths of the capture.  A sparse step is two graphs, with the indexer called between them.
  *
  * Cache.  A pool of pages of LT_PAGE_KEYS = 64 tokens; page p holds, for each of Hkv key-value heads, 64 rows of D + D / 8
  * bytes, so a page takes lt_kv4_page_bytes(Hkv, D) bytes and row `slot` of head h starts at byte
