@@ -299,7 +299,8 @@ int lt_dsa_union_mask(const int32_t* idx, int T, int topk, int N, int group,
  * from query_start[B] on belong to no request: no output is written there (a part of the requests may be given, by pointers into
  * query_start, context_len and page_table).  Positions 64 j .. 64 j + 63 of request b lie in page page_table[b][j].  A position whose table
  * entry is no page of the pool, or lies beyond the table, is seen by no token.  Limits: B <= 2^20, T <= 2^24, max_pages <= 2^24,
- * Hkv <= 1024, fewer than 2^31 rows in the pool.
+ * Hkv <= 1024, fewer than 2^31 rows in the pool.  Single requests may add nothing, but a step without any request or token row (B, T or n
+ * of 0) is LT_ERR_INVALID_ARG in every call.
  * ---------------------------------------------------------------------------------------------
  */
 #define LT_KV4_GROUP 32
@@ -352,7 +353,7 @@ int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t
  * A token that sees nothing gets 0 and -inf.
  *   dtype         LT_DTYPE_BF16 (tensor cores) or LT_DTYPE_F32 (LT_PATH_GENERIC: fp32 arithmetic); type of q and out
  *   q             device: token t's Hq heads of D elements are dense at q + t * q_stride (elements); pointer and rows 16-byte
- *                 aligned.  Hq a multiple of Hkv, T * Hq < 2^31
+ *                 aligned.  Hq a multiple of Hkv, at most 65,535; T * Hq < 2^31
  *   out, lse      device, [T][Hq][D] and [T][Hq] fp32 (or NULL), out 16-byte aligned; not in the memory of any input
  *   max_new       most tokens that any request adds in this step, or 0 if unknown.  It only decides which kernels are
  *                 launched: any value is safe, a right one is fastest
@@ -360,8 +361,11 @@ int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t
  *   workspace     device, 256-byte aligned, at least lt_kv4_attention_workspace_bytes(...) bytes, scratch; one per stream
  *   tunables      path (AUTO, FUSED, GENERIC), grid (SMs to use) and wait_limit_us are used; NULL = defaults
  * q, and the keys and values of positions that some token sees, must be finite; what lies anywhere else in the pool is not
- * used, whatever it is.  Probabilities are rounded to fp16 for the products with the values, everything else is held in fp32;
- * results do not depend on the run (no atomics), but their last bits may on the lengths of the other requests of the batch.
+ * used, whatever it is.  With bf16 queries (but for LT_PATH_GENERIC) probabilities are rounded to fp16 for the products with the values, and a row's
+ * queries are scaled by a power of two to fp16, where a bit that is under 2^-35 of the row's largest element is lost; everything else is held
+ * in fp32.  The fp32 sum of a score's products begins at 8 sum |q| in the kernel of few rows: a score is as near as its largest queries
+ * times their key scales let it be, even if the keys there are zero.
+ * Results do not depend on the run (no atomics), but their last bits may on the lengths of the other requests of the batch.
  */
 int lt_kv4_attention(int dtype, const void* q, long long q_stride, const void* pool, long long pool_pages,
                      const int32_t* page_table, int max_pages, const int32_t* query_start, const int32_t* context_len, int B,

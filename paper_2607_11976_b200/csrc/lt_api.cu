@@ -858,6 +858,9 @@ int lt_kv4_read(int dtype, const void* pool, long long pool_pages, const int32_t
 // 32 rows 62 / 78 / 109, 48: 83 / 83 / 113, 64: 105 / 86 / 116, 128: 184 / 100 / 124, 192: 264 / 152 / 146, 512: 665 / 270 / 259 (2 requests over
 // 16,384: 48 rows 33 / 50 / 56, 128: 58 / 64 / 61, 256: 98 / 69 / 82); 512 tokens of 2 heads over 2048 positions each, few-row / tile:
 // 16 rows 128 / 240, 32: 229 / 246, 48: 328 / 255, 128: 823 / 302.
+// The lines are those of many requests.  They go by rows alone, since the lengths are on the device, and are not the best everywhere: of
+// few long requests the few-row kernel would take 49 to 128 rows up to 1.4 times faster (2 requests over 16,384, 64 rows: 36 against 51), and a
+// pair costs 18 % over a single tile at 256 rows.  The largest request of a batch decides on pairs for all.  For D = 64 they were not measured.
 static constexpr int kKv4FewRows = 48, kKv4FewRowsTopk = 32, kKv4PairRows = 192;
 
 static int kv4_attention_impl(int dtype, const void* q, long long q_stride, const void* pool, long long pool_pages,

@@ -9,8 +9,9 @@
 // row that is picked by itself costs five 32-byte sectors), and 32 rows in a row are one run of memory.
 //
 // The scale is the group's largest magnitude / 7 rounded to bf16, held in fp16, at most 2048.  Its 8 significant bits keep
-// 24 * scale exact in fp16, so that a value comes out of its code with one fp16x2 FMA, (16 + u) * scale - 24 * scale, rounded
-// once: 16 + u is a code with a constant or-ed into its exponent, no conversion.
+// 24 * scale exact in fp16, so that a value comes out of its code with one fp16x2 FMA, (16 + u) * scale - 24 * scale: 16 + u is a code
+// with a constant or-ed into its exponent, no conversion.  Values are exact in fp16 too, subnormal scales included: |u - 8| <= 8 takes
+// 3 more bits at most.  (A scale of more bits that something else put into the pool has its 24-fold and its values rounded.)
 #pragma once
 
 #include <cuda_bf16.h>
@@ -29,7 +30,10 @@ __host__ __device__ constexpr int kv4_row_bytes(int D) { return D + D / 8; }
 
 // Scale of a group from its largest magnitude (both roundings to nearest even).
 __device__ __forceinline__ __half kv4_scale(float amax) {
-  // amax / 7, correctly rounded: a product and its correction (an infinite amax stays as it is)
+  // amax / 7, correctly rounded: a product with 1 / 7 and a correction by its remainder, as in Markstein's division (IBM J. Res. Dev. 34, 1990).
+  // The product is up to 1.15 steps off, more than his theorem allows in general; for this divisor all 2^23 significands were gone through
+  // (a power of two changes nothing): the remainder amax - 7 q is exact, and q + r / 7 rounds to the quotient every time.  (An infinite amax
+  // stays as it is; quotients below the normal range become scales of zero.)
   const float seventh = 1.f / 7.f, q = amax * seventh, r = __fmaf_rn(q, -7.f, amax);
   const float s = __bfloat162float(__float2bfloat16_rn(amax < INFINITY ? __fmaf_rn(r, seventh, q) : amax));
   return __float2half_rn(fminf(s, kKvMaxScale));

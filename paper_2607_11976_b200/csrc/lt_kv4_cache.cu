@@ -160,9 +160,10 @@ __global__ void __launch_bounds__(kTabThreads) page_tables_kernel(const TablePar
 // ---------------------------------------------------------------------------------------------
 // Writer.  A thread takes 8 consecutive elements (one or two 16-byte loads), four threads share a group: two shuffles give its largest
 // magnitude.  16 threads (D = 128) hold a head's keys and the 16 beside them its values, so a warp writes whole rows.  It reads
-// 2 Hkv D elements a token and writes 9 / 16 byte for each; with 16 instructions an element it was bound by those, not by HBM
+// 2 Hkv D elements a token and writes 9 / 16 byte for each; instructions bound it, not HBM.  Quantising alone took 16 an element
 // (65,536 tokens of 8 heads of 128: 200 us), so ordinary groups of bf16 take a shorter way of 6: the quotient by a reciprocal and one
-// correction, the nibble from the bits of a sum that rounds: 98 us, 3.5 TB/s, 0.74 of the issue slots.
+// correction, the nibble from the bits of a sum that rounds.  With walking, addresses, shuffles and stores the kernel still executes 19 an
+// element (80 M warp instructions for 134 M elements): 98 us, 3.5 TB/s, 0.74 of the issue slots.
 // ---------------------------------------------------------------------------------------------
 constexpr int kCacheThreads = 256;
 constexpr int kCacheAhead = 4;  // loads in flight per thread

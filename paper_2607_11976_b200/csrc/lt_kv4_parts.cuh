@@ -65,7 +65,7 @@ __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t c
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "r"(mask), "r"(c));
   return d;
 }
-// Nibble i of each half of w as the fp16 pair (u - 8) s, rounded once; minus24s = -24 s.
+// Nibble i of each half of w as the fp16 pair (u - 8) s; minus24s = -24 s.  Exact for the scales that the writer leaves (lt_kv4.cuh).
 template <int i>
 __device__ __forceinline__ uint32_t f16_values(uint32_t w, uint32_t s, uint32_t minus24s, const ValueConstants& k) {
   if constexpr (i == 0)

@@ -3,7 +3,7 @@
 // An item is up to kTiles tiles of 128 rows (query heads of one key-value head, and tokens) of a request; a CTA takes its keys 128 at a
 // time, or 64 where it has one tile.  Roles, a warp or more each, that meet at mbarriers only:
 //   rows      where the tile's 128 cache rows are (pages, or the indexer's positions), and their copy into a ring of 32 rows a stage
-//   keys      codes from the ring -> fp16 (code - 8) scale, rounded once -> shared memory [key][element], 128-byte swizzle
+//   keys      codes from the ring -> fp16 (code - 8) scale, exact -> shared memory [key][element], 128-byte swizzle
 //   values    the same, transposed: [element][key]
 //   products  one thread: S = Q K^T into tensor memory, O += P V with P as the tensor-memory operand
 //   softmax   a warpgroup per tile, a thread per row: maximum, exponentials, P (fp16) back over S
@@ -60,7 +60,7 @@ struct Shared {
   int b, kvh, rt, unit;
 };
 
-// Items of a request (dense form): row tiles of kRows rows, each with the units of 128 keys that its last row sees.
+// Items of a request (dense form): row tiles of kRows rows, each with the units of kKeys keys that its last row sees.
 template <int kRows, int kKeys>
 __device__ __forceinline__ int item_units(const Kv4AttnParams& p, const Kv4Request& r, int rt) {
   const long long rows = static_cast<long long>(r.n) * p.group, end = static_cast<long long>(rt + 1) * kRows;

@@ -42,16 +42,19 @@ def definition(step, idx=None, device="cpu", times=None):
         t0, t1, ctx = int(step.start[b]), int(step.start[b + 1]), int(step.ctx[b])
         if t1 == t0:
             continue
-        at = torch.arange(ctx + t1 - t0, device=device)
+        at = torch.arange(min(ctx + t1 - t0, 64 * step.table.shape[1]), device=device)
         page = wide(step.table[b].astype(np.int64))[at // 64]
+        there = (page >= 0) & (page < kv[0].shape[0])
+        page = torch.where(there, page, 0)
         last = ctx + torch.arange(t1 - t0, device=device)
         if idx is None:
             count = (at[None] <= last[:, None]).double()
         else:
             i = wide(idx[t0:t1].astype(np.int64))
-            ok = (i >= 0) & (i <= last[:, None])
+            ok = (i >= 0) & (i <= last[:, None]) & (i < at.numel())
             count = torch.zeros(t1 - t0, at.numel(), **rows)
             count.scatter_add_(1, torch.where(ok, i, 0), ok.double())
+        count = count * there
         if times is not None:
             count = count * times[b].to(device)
         for h in range(Hkv):

@@ -77,3 +77,14 @@ def test_the_definition_agrees_with_the_oracle():
         out, lse, spread, weight, mass = kv4.attention(s.q, s.pool, s.table, s.start, s.ctx, s.scale, idx)
         for name, want in (("out", out), ("lse", lse), ("spread", spread), ("mass", mass), ("weight", weight)):
             assert np.allclose(r[name][:5].numpy(), want[:5], rtol=1e-11, atol=1e-12), name
+
+
+def test_the_definition_agrees_with_the_oracle_where_pages_are_missing():
+    s = Step([200, 300], [3, 20], 6, 2, 64, seed=13)
+    s.table[0, 1], s.table[1, 0], s.table[1, 3] = -1, s.pages + 7, 2**31 - 1
+    for cols in (s.table.shape[1], 2):
+        s.table = np.ascontiguousarray(s.table[:, :cols])
+        for idx in (None, s.selection(50, empty_rows=[1], duplicates=True)):
+            r = definition(s, idx)
+            for name, want in zip(("out", "lse"), kv4.attention(s.q, s.pool, s.table, s.start, s.ctx, s.scale, idx)):
+                assert np.allclose(r[name].numpy(), want, rtol=1e-11, atol=1e-12), name
